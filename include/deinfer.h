@@ -309,6 +309,145 @@ int deinfer_lowrank_up_rope(const void *t, int64_t T, int64_t ldt, const deinfer
                             void *ws, size_t ws_bytes, void *stream);
 
 /*
+ * One step of a serving program over a paged cache, from the lengths of its requests to the attention that
+ * reads the cache, with everything that changes between steps in device memory: the calls below can be captured
+ * once, with the largest counts, and replayed.  A step's tokens are rows 0 .. T - 1 of its buffers, sequence after
+ * sequence; T is the buffers' capacity, and the rows behind the last sequence's are padding.  A slot is the index of a
+ * token's row in the pool: block * block_tokens + offset.
+ *
+ * deinfer_kv_step: block tables, slots and positions from the lengths.
+ *   cached, n_new:  device int32 [n_seqs]: tokens that sequence s has in the cache, and how many this step adds
+ *                   (negative counts as 0).  At most DEINFER_KV_MAX_SEQS sequences.
+ *   block_table:    device int32 [n_seqs][table_pitch]; the first ceil(cached / block_tokens) entries of a row are
+ *                   read, those that the new tokens need are written, the rest is left as it is.
+ *   free_list:      device int32 [n_free]: ids of unused blocks; free_first (device int32, may be NULL: 0): the first
+ *                   entry to use.  Sequences take blocks in order; the list itself is not changed, so a step can be
+ *                   repeated.  An id outside [0, n_pool_blocks) becomes -1 in the table.
+ *   row_start:      device int32 [n_seqs + 1], out: first row of every sequence, and the end of the last.
+ *   slots, positions: device int32 [T], out: slot of a row's token (-1: padding, or no block was left for it or no room
+ *                   in the table), and its position, cached + its index (padding: 0).
+ *   counts:         device int32 [4], out: [0] new tokens in all (more than T: the rest has no rows and gets no
+ *                   blocks), [1] blocks taken, [2] blocks that were needed and not to be had, [3] free_first + [1].
+ * free_first must not point into counts (copy counts[3] to it between steps).
+ */
+#define DEINFER_KV_MAX_SEQS 8192
+int deinfer_kv_step(const int32_t *cached, const int32_t *n_new, int64_t n_seqs,
+                    const int32_t *free_list, int64_t n_free, const int32_t *free_first,
+                    int64_t n_pool_blocks, int64_t block_tokens,
+                    int32_t *block_table, int64_t table_pitch, int64_t T,
+                    int32_t *row_start, int32_t *slots, int32_t *positions, int32_t *counts,
+                    void *stream);
+
+/*
+ * deinfer_kv_compact_plan_device: the scan of deinfer_kv_compact_plan on the device, so that a step whose block
+ * tables are made on the device needs no host in between.  Every array is a device array; sequence s holds
+ * n_tokens[s] (+ n_new[s], where n_new is not NULL) tokens, i.e. that many tokens' blocks rounded up.  plan, remap,
+ * positions as there, all of them written in full (runs beyond the last: zeros).  What the host call refuses is told
+ * in plan[2], as a sum of the flags below, and then plan[0] = plan[1] = 0, so that the copy moves nothing;
+ * remap is -1 for blocks outside the pool or beyond the buffer.
+ */
+enum {
+  DEINFER_KV_PLAN_BAD_BLOCK = 1,   /* a block id outside [0, n_pool_blocks) */
+  DEINFER_KV_PLAN_BUFFER_FULL = 2, /* more blocks than the buffer holds */
+  DEINFER_KV_PLAN_TABLE_FULL = 4,  /* a sequence with more blocks than a row of block_table or remap holds */
+  DEINFER_KV_PLAN_RUNS_FULL = 8    /* more runs than plan_capacity_runs */
+};
+int deinfer_kv_compact_plan_device(const int32_t *block_table, int64_t n_seqs, int64_t table_pitch,
+                                   const int32_t *n_tokens, const int32_t *n_new,
+                                   int64_t n_pool_blocks, int64_t buffer_blocks, int64_t block_tokens,
+                                   int32_t *plan, int64_t plan_capacity_runs,
+                                   int32_t *remap, int64_t remap_pitch, int32_t *positions, void *stream);
+
+/*
+ * deinfer_tree_mask: what the tokens of drafted trees see of each other, from their parents.
+ *   parents:   device int32 [T]: index, among its sequence's rows, of the token that a row's token follows; anything
+ *              outside [0, its own index): it follows the cached text.
+ *   row_start, cached: as of deinfer_kv_step.
+ *   mask:      device uint32 [T][mask_words], out: bit j of a row (bit j % 32 of word j / 32) is set if the row's token
+ *              sees token j of its sequence's rows: its ancestors and itself.  mask_words <= DEINFER_TREE_MAX_WORDS;
+ *              rows beyond the 32 mask_words-th of a sequence get no bits.
+ *   positions: device int32 [T], out, may be NULL: cached + number of ancestors.
+ * Padding rows are left as they are.
+ */
+#define DEINFER_TREE_MAX_WORDS 32
+int deinfer_tree_mask(const int32_t *parents, const int32_t *row_start, const int32_t *cached,
+                      int64_t n_seqs, int64_t T, uint32_t *mask, int64_t mask_words,
+                      int32_t *positions, void *stream);
+
+/*
+ * deinfer_rope_frequencies (host only): freqs[i], i < rot_dim / 2, the angle per position of pair i, from
+ * f_i = theta^(-2 i / rot_dim) and one of the usual ways to serve contexts longer than those of the training:
+ *   PLAIN   f_i
+ *   LINEAR  f_i / factor (positions interpolated)
+ *   BASE    theta replaced by theta factor^(D / (D - 2)), D = rot_dim: the fastest pair keeps its frequency, the slowest is
+ *           divided by factor
+ *   BANDS   by the turns r = original_context f_i / (2 pi) within the original context: f_i for r >= high,
+ *           f_i / factor for r <= low, in between (1 - b) f_i / factor + b f_i with b = (r - low) / (high - low)
+ *   RAMP    the same blend, linear in the pair's index from the pair that turns `high` times (rounded down) to the one that
+ *           turns `low` times (rounded up); *magnitude = 0.1 ln(factor) + 1 for factor > 1
+ * *magnitude (may be NULL): factor of the rotated elements; 1 but for RAMP.
+ *
+ * deinfer_rope_store: rotary embedding of a step's queries and keys, and the way of keys and values into the cache, in
+ * one launch.  For every row t and head, the pairs (i, i + rot_dim / 2), or (2 i, 2 i + 1) if interleaved is not 0,
+ * i < rot_dim / 2, are rotated by the angle positions[t] freqs[i] and multiplied by magnitude; elements from rot_dim on
+ * are copied.
+ *   q -> q_out     T x (n_q_heads head_dim), pitches ldq, ldqo; q_out may be q.  Both NULL: no queries.
+ *   k -> k_out, v -> v_out   T x (n_kv_heads head_dim); v is copied.  Each pair may be NULL.  With slots (device int32
+ *                  [T]) row t goes to row slots[t] of k_out and v_out (n_slots rows: the pools); rows whose slot is
+ *                  outside [0, n_slots) are skipped, their queries too.  Slots in use have to differ.  Without slots row
+ *                  t goes to row t, and k_out may be k, v_out v.
+ *   positions      device int32 [T]; freqs: device double [rot_dim / 2].  rot_dim = 0 only copies (rows of the low-rank cache).
+ * dtype: of q, k, v and the outputs.  Any pitches and alignments; 16-byte aligned rows, head_dim and rot_dim / 2 (rot_dim
+ * where interleaved) of whole 16-byte pieces take 16-byte loads and stores.  Angles in double precision, products in
+ * fp32, one rounding.
+ */
+enum { DEINFER_ROPE_PLAIN = 0, DEINFER_ROPE_LINEAR = 1, DEINFER_ROPE_BASE = 2, DEINFER_ROPE_BANDS = 3, DEINFER_ROPE_RAMP = 4 };
+typedef struct deinfer_rope_scaling {
+  int32_t kind;                    /* DEINFER_ROPE_... */
+  double factor;                   /* not PLAIN */
+  double original_context;         /* BANDS, RAMP: positions of the training */
+  double low, high;                /* BANDS, RAMP: turns; low < high */
+} deinfer_rope_scaling_t;
+int deinfer_rope_frequencies(int64_t rot_dim, double theta, const deinfer_rope_scaling_t *scaling,
+                             double *freqs, double *magnitude);
+int deinfer_rope_store(const void *q, int64_t ldq, int64_t n_q_heads,
+                       const void *k, int64_t ldk, const void *v, int64_t ldv, int64_t n_kv_heads,
+                       int64_t T, int64_t head_dim, int64_t rot_dim, int interleaved,
+                       const int32_t *positions, const double *freqs, double magnitude,
+                       const int32_t *slots, int64_t n_slots,
+                       void *q_out, int64_t ldqo, void *k_out, int64_t ldko, void *v_out, int64_t ldvo,
+                       int dtype, void *stream);
+
+/*
+ * deinfer_tree_attention: attention of a step's tokens over the paged cache, their own keys and values among it
+ * (deinfer_rope_store has put them there; or rebuilt keys and values in a compact buffer, with the remapped table of the
+ * plan): one token per sequence, drafted trees, chunks of prompts.
+ *   out[t, h] = sum_j p_j v_j, p = softmax over the keys j that row t sees of scale (q[t, h] . k_j)
+ * where query head h reads key head h / (n_q_heads / n_kv_heads).  Row i of sequence s (rows row_start[s] ..
+ * row_start[s + 1] - 1) sees the cached[s] tokens before it and, of its sequence's rows, those in its bits of mask (as
+ * deinfer_tree_mask makes them; any bits are taken as they are; rows without a bit in mask_words words are not
+ * seen); mask = NULL: the rows up to its own.  A row that sees no key gives zeros.  Keys in blocks whose id is
+ * outside [0, n_pool_blocks), and those beyond the table's row, are not seen.  What a row does not see has no
+ * influence, infinities and NaN included.  Padding rows of out are left as they are.
+ *   q, out: T x (n_q_heads head_dim), pitches ldq, ldo; k_pool, v_pool: n_pool_blocks * block_tokens rows of n_kv_heads
+ *   head_dim, pitches ldk, ldv; block_table: device int32 [n_seqs][table_pitch], at least ceil((cached + rows) /
+ *   block_tokens) entries of a row in use.  dtype: bf16 or fp16.  head_dim: a multiple of 8, at most 256.  scale > 0.
+ *   q, pools and out 16-byte aligned, pitches multiples of 8.  out must not overlap q.
+ * Scores, maxima, sums and outputs are fp32; the probabilities are rounded to the storage type for the second product, the
+ * output is rounded once.  Results do not depend on timing.  The workspace (deinfer_tree_attention_workspace_bytes,
+ * host only; 256-byte aligned) needs no clearing and serves one call at a time.  T <= 2^28, T n_q_heads < 2^30.
+ */
+int deinfer_tree_attention_workspace_bytes(int64_t T, int64_t n_seqs, int64_t n_q_heads, int64_t n_kv_heads,
+                                           int64_t head_dim, size_t *bytes);
+int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads,
+                           int64_t head_dim, const int32_t *row_start, const int32_t *cached, int64_t n_seqs,
+                           const uint32_t *mask, int64_t mask_words,
+                           const void *k_pool, int64_t ldk, const void *v_pool, int64_t ldv,
+                           int64_t n_pool_blocks, int64_t block_tokens,
+                           const int32_t *block_table, int64_t table_pitch, double scale,
+                           void *out, int64_t ldo, int dtype, void *ws, size_t ws_bytes, void *stream);
+
+/*
  * MLP second sub-layer (Sec. 4.1): y = (h U_d) V_d with d_in = FFN width.
  * Same contract as deinfer_lowrank_linear.
  */

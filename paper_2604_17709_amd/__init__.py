@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Sequence
+from typing import Any, NamedTuple, Optional, Sequence
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 # DEINFER_LIBRARY_PATH names another build of the library to load (e.g. the host-sanitized one of build.py)
@@ -46,6 +46,12 @@ class Factors(ctypes.Structure):
                 ("param_reduction", ctypes.c_double)]
 
 
+class RopeScaling(ctypes.Structure):
+    """Mirror of ``deinfer_rope_scaling_t``."""
+    _fields_ = [("kind", ctypes.c_int32), ("factor", ctypes.c_double), ("original_context", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double)]
+
+
 class DeinferError(RuntimeError):
     def __init__(self, code: int, text: str):
         super().__init__(f"deinfer error {code}: {text}")
@@ -65,6 +71,8 @@ EXPORTS = [
     "deinfer_lowrank_down_proj", "deinfer_lowrank_up_glu_silu",
     "deinfer_kv_compact_plan", "deinfer_kv_compact_copy", "deinfer_rope_inplace",
     "deinfer_rope_table", "deinfer_lowrank_up_rope",
+    "deinfer_kv_step", "deinfer_kv_compact_plan_device", "deinfer_tree_mask", "deinfer_rope_frequencies", "deinfer_rope_store",
+    "deinfer_tree_attention_workspace_bytes", "deinfer_tree_attention",
 ]
 
 _lib = None
@@ -118,6 +126,16 @@ def lib() -> ctypes.CDLL:
                                           _vp, _i64, _vp, _i64, _vp, _i64,
                                           _vp, _i64, _vp, _i64, _vp, _sz, _vp]
         L.deinfer_lowrank_gateup_silu.argtypes = [_vp, _i64, _i64, FP, FP, _vp, _i64, _vp, _sz, _vp]
+        L.deinfer_kv_step.argtypes = [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp]
+        L.deinfer_kv_compact_plan_device.argtypes = [_vp, _i64, _i64, _vp, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp]
+        L.deinfer_tree_mask.argtypes = [_vp, _vp, _vp, _i64, _i64, _vp, _i64, _vp, _vp]
+        _dp = ctypes.POINTER(ctypes.c_double)
+        L.deinfer_rope_frequencies.argtypes = [_i64, ctypes.c_double, ctypes.POINTER(RopeScaling), _dp, _dp]
+        L.deinfer_rope_store.argtypes = [_vp, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _i64, _i64, ctypes.c_int, _vp, _vp, ctypes.c_double,
+                                         _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, ctypes.c_int, _vp]
+        L.deinfer_tree_attention_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64, _i64, ctypes.POINTER(_sz)]
+        L.deinfer_tree_attention.argtypes = [_vp, _i64, _i64, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64,
+                                             _vp, _i64, ctypes.c_double, _vp, _i64, ctypes.c_int, _vp, _sz, _vp]
         for name in EXPORTS:
             if name not in ("deinfer_last_error",):
                 getattr(L, name).restype = ctypes.c_int
@@ -502,4 +520,208 @@ def deinfer_lowrank_gateup_silu(x, fgate: Pair, fup: Pair, ws: Workspace, out=No
     _check(lib().deinfer_lowrank_gateup_silu(_ptr(x), T, _ld(x), ctypes.byref(fgate.desc),
                                              ctypes.byref(fup.desc), _ptr(out), _ld(out),
                                              _ptr(ws.buf), ws.nbytes, _stream(stream)))
+    return out
+
+
+# ------------------------------------------------------------------ one step over a paged cache
+def _on_device(*tensors) -> None:
+    """The library takes pointers of the current device: anything else is refused here, before a kernel reads it."""
+    import torch
+    here = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"tensors of the current device (cuda:{here}) expected, got one on {t.device}")
+
+
+def _ints(what: str, t, n: Optional[int] = None):
+    """A contiguous int32 list of at least n values."""
+    import torch
+    if t.dtype != torch.int32 or not t.is_contiguous() or (n is not None and t.numel() < n):
+        raise ValueError(f"{what}: contiguous int32 tensor{'' if n is None else f' of at least {n} values'} expected")
+    return t
+
+
+def _table(t, n_seqs: int) -> int:
+    """Pitch of a block table [n_seqs, pitch]."""
+    _ints("block_table", t)
+    if t.dim() != 2 or t.shape[0] < n_seqs:
+        raise ValueError("block_table: [n_seqs, pitch] expected")
+    return t.shape[1]
+
+
+def _new(shape, dtype, device, stream):
+    """An output that belongs to the stream that will write it."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class KvStep(NamedTuple):
+    """What ``deinfer_kv_step`` writes beside the block table."""
+    row_start: Any      # [n_seqs + 1]
+    slots: Any          # [rows]
+    positions: Any      # [rows]
+    counts: Any         # [4]
+
+
+def deinfer_kv_step(cached, n_new, block_table, free_list, block_tokens: int, n_pool_blocks: int, rows: int, free_first=None,
+                    out: Optional[KvStep] = None, stream=None) -> KvStep:
+    """Block tables (updated in place), slots and positions of a step's tokens from the requests' lengths."""
+    import torch
+    n = cached.numel()
+    _ints("cached", cached)
+    _ints("n_new", n_new, n)
+    _ints("free_list", free_list)
+    pitch = _table(block_table, n)
+    if free_first is not None:
+        _ints("free_first", free_first, 1)
+    if out is None:
+        out = KvStep(*(_new(k, torch.int32, cached.device, stream) for k in (n + 1, int(rows), int(rows), 4)))
+    for name, t, k in zip(KvStep._fields, out, (n + 1, rows, rows, 4)):
+        _ints(name, t, k)
+    _on_device(cached, n_new, block_table, free_list, free_first, *out)
+    _check(lib().deinfer_kv_step(_ptr(cached), _ptr(n_new), n, _ptr(free_list), free_list.numel(), _ptr(free_first), int(n_pool_blocks),
+                                 int(block_tokens), _ptr(block_table), pitch, int(rows), _ptr(out.row_start), _ptr(out.slots),
+                                 _ptr(out.positions), _ptr(out.counts), _stream(stream)))
+    return out
+
+
+def deinfer_kv_compact_plan_device(block_table, n_tokens, n_pool_blocks: int, buffer_blocks: int, block_tokens: int, n_new=None,
+                                   capacity_runs: Optional[int] = None, out=None, stream=None):
+    """``deinfer_kv_compact_plan`` on the device: (plan, remap, positions) from the device's block table and lengths."""
+    import torch
+    n = n_tokens.numel()
+    _ints("n_tokens", n_tokens)
+    pitch = _table(block_table, n)
+    if n_new is not None:
+        _ints("n_new", n_new, n)
+    if out is None:
+        cap = int(buffer_blocks if capacity_runs is None else capacity_runs)
+        dev = n_tokens.device
+        out = (_new(KV_PLAN_HEADER + 3 * cap, torch.int32, dev, stream), _new((n, pitch), torch.int32, dev, stream),
+               _new(int(buffer_blocks) * int(block_tokens), torch.int32, dev, stream))
+    plan, remap, positions = out
+    _ints("plan", plan, KV_PLAN_HEADER)
+    if remap is not None:
+        _table(remap, n)
+    if positions is not None:
+        _ints("positions", positions, int(buffer_blocks) * int(block_tokens))
+    _on_device(block_table, n_tokens, n_new, plan, remap, positions)
+    _check(lib().deinfer_kv_compact_plan_device(_ptr(block_table), n, pitch, _ptr(n_tokens), _ptr(n_new), int(n_pool_blocks),
+                                                int(buffer_blocks), int(block_tokens), _ptr(plan), (plan.numel() - KV_PLAN_HEADER) // 3,
+                                                _ptr(remap), 0 if remap is None else remap.shape[1], _ptr(positions), _stream(stream)))
+    return plan, remap, positions
+
+
+def deinfer_tree_mask(parents, row_start, cached, mask, positions=None, stream=None):
+    """Visibility bits (int32 [rows, words], bit patterns) and positions of drafted trees from their tokens' parents."""
+    n, rows = cached.numel(), parents.numel()
+    _ints("parents", parents)
+    _ints("cached", cached)
+    _ints("row_start", row_start, n + 1)
+    _ints("mask", mask)
+    if mask.dim() != 2 or mask.shape[0] < rows:
+        raise ValueError("mask: [rows, words] expected")
+    if positions is not None:
+        _ints("positions", positions, rows)
+    _on_device(parents, row_start, cached, mask, positions)
+    _check(lib().deinfer_tree_mask(_ptr(parents), _ptr(row_start), _ptr(cached), n, rows, _ptr(mask), mask.shape[1], _ptr(positions),
+                                   _stream(stream)))
+    return mask, positions
+
+
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3, 4
+
+
+def deinfer_rope_frequencies(rot_dim: int, theta: float = 10000.0, kind: int = ROPE_PLAIN, factor: float = 1.0, original_context: float = 0.0,
+                             low: float = 0.0, high: float = 0.0):
+    """(frequencies, magnitude) of the rotated pairs (host): float64 numpy [rot_dim / 2], for contexts scaled as ``kind`` says."""
+    import numpy as np
+    freqs = np.zeros(max(int(rot_dim), 2) // 2, dtype=np.float64)
+    magnitude = ctypes.c_double(1.0)
+    sc = RopeScaling(int(kind), float(factor), float(original_context), float(low), float(high))
+    _check(lib().deinfer_rope_frequencies(int(rot_dim), float(theta), ctypes.byref(sc), freqs.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
+                                          ctypes.byref(magnitude)))
+    return freqs, float(magnitude.value)
+
+
+def deinfer_rope_store(q, k, v, positions, freqs, n_q_heads: int, n_kv_heads: int, head_dim: int, interleaved: bool = False,
+                       magnitude: float = 1.0, slots=None, q_out=None, k_out=None, v_out=None, stream=None):
+    """Queries rotated, keys rotated and values copied into their slots of the cache.  q, k and v may each be None; q_out, k_out
+    and v_out default to them (k and v: without slots only).  freqs: float64 device tensor [rot_dim / 2], or None to copy."""
+    import torch
+    given = [t for t in (q, k, v) if t is not None]
+    if not given:
+        return q_out, k_out, v_out
+    rows = _rows(given[0], "rows")
+    q_out = q if q_out is None else q_out
+    if slots is None:
+        k_out, v_out = (k if k_out is None else k_out), (v if v_out is None else v_out)
+    elif (k is not None and k_out is None) or (v is not None and v_out is None):
+        raise ValueError("with slots, k_out and v_out (the pools) are needed")
+    n_slots = None
+    for what, t, to, heads in (("q", q, q_out, n_q_heads), ("k", k, k_out, n_kv_heads), ("v", v, v_out, n_kv_heads)):
+        if t is None:
+            continue
+        pooled = slots is not None and what != "q"
+        if _rows(t, what) != rows or t.shape[1] < heads * head_dim or to.dtype != t.dtype or t.dtype != given[0].dtype:
+            raise ValueError(f"{what}: [rows, heads * head_dim] of one dtype expected")
+        if _rows(to, what + "_out") < (0 if pooled else rows) or to.shape[1] < heads * head_dim:
+            raise ValueError(f"{what}_out: too small")
+        if pooled:
+            n_slots = to.shape[0] if n_slots is None else min(n_slots, to.shape[0])
+    if freqs is not None and (freqs.dtype != torch.float64 or not freqs.is_contiguous()):
+        raise ValueError("freqs: contiguous float64 tensor expected")
+    if freqs is not None and freqs.numel():
+        _ints("positions", positions, rows)
+    if slots is not None:
+        _ints("slots", slots, rows)
+    _on_device(q, k, v, positions, freqs, slots, q_out if q is not None else None, k_out if k is not None else None, v_out if v is not None else None)
+    p = lambda t, to: (None, 0, None, 0) if t is None else (_ptr(t), _ld(t), _ptr(to), _ld(to))
+    (qp, ldq, qo, ldqo), (kp, ldk, ko, ldko), (vp, ldv, vo, ldvo) = p(q, q_out), p(k, k_out), p(v, v_out)
+    _check(lib().deinfer_rope_store(qp, ldq, int(n_q_heads), kp, ldk, vp, ldv, int(n_kv_heads), rows, int(head_dim),
+                                    0 if freqs is None else 2 * freqs.numel(), int(interleaved), _ptr(positions), _ptr(freqs), float(magnitude),
+                                    _ptr(slots), n_slots or 0, qo, ldqo, ko, ldko, vo, ldvo, _dtype_code(given[0]), _stream(stream)))
+    return q_out, k_out, v_out
+
+
+def deinfer_tree_attention_workspace_bytes(rows: int, n_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    n = _sz(0)
+    _check(lib().deinfer_tree_attention_workspace_bytes(int(rows), int(n_seqs), int(n_q_heads), int(n_kv_heads), int(head_dim), ctypes.byref(n)))
+    return int(n.value)
+
+
+def deinfer_tree_attention(q, k_pool, v_pool, block_table, row_start, cached, ws: Workspace, n_q_heads: int, n_kv_heads: int, block_tokens: int,
+                           scale: Optional[float] = None, mask=None, out=None, stream=None):
+    """Attention of a step's rows over the paged cache: k_pool, v_pool [slots, n_kv_heads * head_dim]; mask: int32 [rows, words]
+    visibility bits among a sequence's own rows (None: causal).  Rows behind the last sequence's keep what ``out`` holds."""
+    rows, n = _rows(q, "q"), cached.numel()
+    if n_q_heads <= 0 or q.shape[1] % n_q_heads:
+        raise ValueError("q: [rows, n_q_heads * head_dim] expected")
+    head_dim = q.shape[1] // n_q_heads
+    n_slots = _rows(k_pool, "k_pool")
+    if _rows(v_pool, "v_pool") != n_slots or k_pool.shape[1] < n_kv_heads * head_dim or v_pool.shape[1] < n_kv_heads * head_dim:
+        raise ValueError("k_pool, v_pool: [slots, n_kv_heads * head_dim] expected")
+    if k_pool.dtype != q.dtype or v_pool.dtype != q.dtype:
+        raise ValueError("q, k_pool and v_pool must share a dtype")
+    _ints("cached", cached)
+    _ints("row_start", row_start, n + 1)
+    pitch = _table(block_table, n)
+    words = 0
+    if mask is not None:
+        _ints("mask", mask)
+        if mask.dim() != 2 or mask.shape[0] < rows:
+            raise ValueError("mask: [rows, words] expected")
+        words = mask.shape[1]
+    if out is None:
+        out = _new((rows, n_q_heads * head_dim), q.dtype, q.device, stream)
+    elif out.dtype != q.dtype or _rows(out, "out") < rows or out.shape[1] < n_q_heads * head_dim:
+        raise ValueError("out: [rows, n_q_heads * head_dim] of q's dtype expected")
+    _on_device(q, k_pool, v_pool, block_table, row_start, cached, mask, out, ws.buf)
+    _check(lib().deinfer_tree_attention(_ptr(q), rows, _ld(q), int(n_q_heads), int(n_kv_heads), head_dim, _ptr(row_start), _ptr(cached), n,
+                                        _ptr(mask), words, _ptr(k_pool), _ld(k_pool), _ptr(v_pool), _ld(v_pool), n_slots // int(block_tokens),
+                                        int(block_tokens), _ptr(block_table), pitch, head_dim ** -0.5 if scale is None else float(scale),
+                                        _ptr(out), _ld(out), _dtype_code(q), _ptr(ws.buf), ws.nbytes, _stream(stream)))
     return out

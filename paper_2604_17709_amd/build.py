@@ -1,4 +1,4 @@
-"""Build step of the HIP library: one hipcc invocation, gfx950 only, in-tree output.
+"""Build step of the HIP library: one hipcc invocation per source, side by side, and one that links; gfx950 only, in-tree output.
 
     python -m paper_2604_17709_amd.build          # compile libdeinfer.so next to this file
 
@@ -10,13 +10,14 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdeinfer.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-munsafe-fp-atomics",
     # keep the compiler from forming packed-fp32 instructions
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -32,7 +33,7 @@ def hipcc() -> str:
 
 
 def sources():
-    return [os.path.join(CSRC, "deinfer_api.hip")]
+    return [os.path.join(CSRC, "deinfer_api.hip"), os.path.join(CSRC, "cache_step_api.hip")]
 
 
 SAN_LIB = os.path.join(HERE, "libdeinfer_hostsan.so")
@@ -64,15 +65,23 @@ def build_host_sanitized(verbose: bool = False) -> str:
 
 def build_library(verbose: bool = False, extra_flags=(), out: str = LIB, check_load: bool = True) -> str:
     LIB = out
-    cmd = [hipcc(), *HIPCC_FLAGS, *extra_flags, "-I", os.path.join(os.path.dirname(HERE), "include"),
-           "-o", LIB + ".tmp", *sources()]
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    flags = [hipcc(), *HIPCC_FLAGS, *extra_flags, "-I", os.path.join(os.path.dirname(HERE), "include")]
+    with tempfile.TemporaryDirectory(prefix="deinfer_build_") as tmp:
+        objects = [os.path.join(tmp, os.path.basename(src) + ".o") for src in sources()]
+        jobs = [[*flags, "-c", src, "-o", obj] for src, obj in zip(sources(), objects)]
+        running = [subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True) for cmd in jobs]
+        results = [(cmd, p.communicate()[1], p.returncode) for cmd, p in zip(jobs, running)]
+        if all(rc == 0 for _, _, rc in results):
+            link = [*flags, "-shared", "-o", LIB + ".tmp", *objects]
+            res = subprocess.run(link, capture_output=True, text=True)
+            results.append((link, res.stderr, res.returncode))
     noise = "is not a recognized feature for this target"
-    err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + " ".join(cmd) + "\n" + err)
-    if verbose and err.strip():
-        print(err, file=sys.stderr)
+    for cmd, text, rc in results:
+        err = "\n".join(l for l in text.splitlines() if noise not in l)
+        if rc != 0:
+            raise RuntimeError("hipcc failed:\n" + " ".join(cmd) + "\n" + err)
+        if verbose and err.strip():
+            print(err, file=sys.stderr)
     # a missing host stub or symbol shows up only at load time: check before replacing the old build
     if check_load:
         import ctypes

@@ -12,6 +12,7 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kWave = 64;
+constexpr int KV_PLAN_HEADER = 4;            // plan of the compacting copy: int32 words before the (src, dst, length) triples
 
 // ---- bf16 <-> fp32 (storage type is a raw 16-bit pattern) -------------------
 __device__ __forceinline__ float bf16_to_f32(uint16_t b) {

@@ -23,6 +23,7 @@
 #include "stream_kernel.h"
 #include "probe_kernels.h"
 #include "paged_kernels.h"
+#include "host_common.h"
 
 using namespace deinfer;
 
@@ -46,6 +47,12 @@ struct ProfScope {
   ~ProfScope() { if (on) (void)hipEventRecord(g_prof_ev[1], s); }
 };
 
+static_assert(DT_BF16 == DEINFER_BF16 && DT_F16 == DEINFER_F16, "the kernels' storage-type codes are the boundary's dtype codes");
+}  // namespace
+
+// ---- what the other host sources of the library use too (host_common.h)
+namespace deinfer {
+
 int fail(int code, const char *fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
@@ -54,18 +61,28 @@ int fail(int code, const char *fmt, ...) {
   return code;
 }
 
-inline int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline size_t elem_size(int dtype) { return dtype == DEINFER_F32 ? 4 : 2; }
-static_assert(DT_BF16 == DEINFER_BF16 && DT_F16 == DEINFER_F16, "the kernels' storage-type codes are the boundary's dtype codes");
-// Calls f with a value of the element type of `dtype` (float, uint16_t for bf16, f16_bits for fp16).
-template <typename F>
-int by_dtype(int dtype, F f) {
-  if (dtype == DEINFER_F32) return f(float{});
-  if (dtype == DEINFER_F16) return f(f16_bits{});
-  return f(uint16_t{});
+int device_cus() {
+  static std::atomic<int> cached[64];       // (threads may race to fill an entry: they store the same value)
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return -1;
+  if (dev < 0 || dev >= 64) return -1;
+  int n = cached[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) return -1;
+    cached[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
 }
-inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+int check_launch(const char *what) {
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(DEINFER_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
+  return DEINFER_OK;
+}
+
+}  // namespace deinfer
+
+namespace {
 
 // ---- workspace layout -------------------------------------------------------------
 // [0, 256)   status words (reserved; cleared by deinfer_workspace_init)
@@ -97,19 +114,6 @@ Geometry geometry(const deinfer_factors_t *f) {
   g.u_bytes = (size_t)g.n_rtiles * g.KB1 * 1024;
   g.v_bytes = (size_t)g.n_otiles * g.KB2 * 1024;
   return g;
-}
-
-int device_cus() {
-  static std::atomic<int> cached[64];       // (threads may race to fill an entry: they store the same value)
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess) return -1;
-  if (dev < 0 || dev >= 64) return -1;
-  int n = cached[dev].load(std::memory_order_relaxed);
-  if (n == 0) {
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) return -1;
-    cached[dev].store(n, std::memory_order_relaxed);
-  }
-  return n;
 }
 
 // ---- split of a memory-bound call with 16 < T <= 128 tokens
@@ -329,12 +333,6 @@ size_t workspace_need(int64_t T, const deinfer_factors_t *const *pairs, int n, s
     if (reduced > need) need = reduced;
   }
   return need;
-}
-
-int check_launch(const char *what) {
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(DEINFER_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
-  return DEINFER_OK;
 }
 
 template <typename TC>

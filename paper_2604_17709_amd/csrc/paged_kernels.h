@@ -7,7 +7,6 @@
 
 namespace deinfer {
 
-constexpr int KV_PLAN_HEADER = 4;            // int32 words before the (src, dst, length) triples
 constexpr int KV_COPY_THREADS = 256;
 constexpr int KV_PIECE = KV_COPY_THREADS * 4 * 16;   // bytes one workgroup moves per step (16 KiB)
 constexpr int KV_LDS_RUNS = 2048;            // run destinations a workgroup keeps in LDS (8 KiB)

@@ -1,0 +1,365 @@
+// One step of a paged cache, from the lengths of the requests: block tables, slots and positions of
+// the step's tokens, the plan of the compacting copy, and the visibility bits of drafted trees.
+//
+// All of these are whole-number work of a few bytes per token; what bounds them is the latency of one
+// launch (a dependent chain of: lengths from memory, prefix sums over the sequences, a bisection in
+// LDS, one load of a block id, the stores).  So each is one launch without hand-over between
+// workgroups: every workgroup forms the prefix sums of all sequences by itself in its LDS
+// (at most STEP_MAX_SEQS sequences, a few KiB that come from the caches), which costs less than a
+// second launch and needs no scratch memory.
+#pragma once
+#include "common.h"
+
+namespace deinfer {
+
+constexpr int STEP_THREADS = 1024;
+constexpr int STEP_MAX_SEQS = 8192;
+constexpr int STEP_ROWS = 4;                     // consecutive rows of one thread: one bisection, 16-byte stores
+
+// inclusive sum over the workgroup's threads; total: the sum of all.  scratch: STEP_THREADS / 64 values
+template <typename TV> __device__ __forceinline__ TV block_scan(TV v, TV *scratch, TV *total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const TV u = __shfl_up(v, o, 64);
+    if (lane >= o) v += u;
+  }
+  __syncthreads();                               // (scratch of the previous call is read)
+  if (lane == 63) scratch[wave] = v;
+  __syncthreads();
+  TV before = 0, all = 0;
+  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) {
+    const TV u = scratch[w];
+    if (w < wave) before += u;
+    all += u;
+  }
+  *total = all;
+  return v + before;
+}
+
+// last index s in [0, n] with start[s] <= x, where start[0] <= x (start has n + 1 ascending entries)
+__device__ __forceinline__ int last_not_above(const int *start, int n, int x) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (start[mid] <= x) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+struct KvStepParams {
+  const int *cached, *n_new, *free_list, *free_first;
+  int *table, *row_start, *slots, *positions, *counts;
+  long long table_pitch, n_free, n_pool_blocks;
+  int n_seqs, block_tokens, T;
+  bool vec;                                      // slots and positions are 16-byte aligned
+};
+
+// Sequence s holds c tokens and gets m: rows row_start[s] + j, positions c + j, j < m.  Its blocks
+// ceil(c / b) .. ceil((c + m) / b) - 1 are new; the new blocks of all sequences, counted in order, take
+// the free list's entries in order.  Entries of the table below ceil(c / b) are read, those from there
+// on are written, so no workgroup reads what another writes; a new block is written by the row of
+// its first token.
+__global__ __launch_bounds__(STEP_THREADS) void kv_step_kernel(const KvStepParams P) {
+  __shared__ int row_start[STEP_MAX_SEQS + 1];
+  __shared__ int need_start[STEP_MAX_SEQS + 1];
+  __shared__ long long scratch64[STEP_THREADS / 64];
+  __shared__ int scratch[STEP_THREADS / 64];
+  const int n = P.n_seqs, bt = P.block_tokens;
+  long long rows_before = 0, wanted = 0;         // wanted: blocks that the sequences need, whether the table has room or not
+  int need_before = 0;
+  for (int s0 = 0; s0 < n; s0 += STEP_THREADS) {
+    const int s = s0 + (int)threadIdx.x;
+    long long c = 0, m = 0;
+    if (s < n) {
+      c = P.cached[s]; m = P.n_new[s];
+      c = c < 0 ? 0 : c; m = m < 0 ? 0 : m;
+    }
+    long long total;
+    const long long end = rows_before + block_scan(m, scratch64, &total);
+    rows_before += total;
+    const int e = (int)(end < P.T ? end : P.T), b = (int)(end - m < P.T ? end - m : P.T);
+    const long long first = (c + bt - 1) / bt, last = (c + (e - b) + bt - 1) / bt;
+    const int need = (int)((last < P.table_pitch ? last : P.table_pitch) - (first < P.table_pitch ? first : P.table_pitch));
+    int need_total;
+    const int need_end = need_before + block_scan(need, scratch, &need_total);
+    need_before += need_total;
+    wanted += last - first;                      // (this thread's sequences; summed below)
+    if (s < n) { row_start[s] = b; need_start[s] = need_end - need; }
+  }
+  const int rows = (int)(rows_before < P.T ? rows_before : P.T);
+  if (threadIdx.x == 0) row_start[n] = rows;
+  const long long free_first = P.free_first ? *P.free_first : 0;
+  long long have = P.n_free - free_first;        // entries that may be taken
+  if (free_first < 0 || have < 0) have = 0;
+  __syncthreads();
+  if (blockIdx.x == 0) {
+    for (int s = threadIdx.x; s <= n; s += STEP_THREADS) P.row_start[s] = row_start[s];
+    long long all;
+    block_scan(wanted, scratch64, &all);
+    if (threadIdx.x == 0) {
+      const long long taken = need_before < have ? need_before : have;
+      P.counts[0] = (int)(rows_before < INT32_MAX ? rows_before : INT32_MAX);
+      P.counts[1] = (int)taken;
+      P.counts[2] = (int)(all - taken < INT32_MAX ? all - taken : INT32_MAX);
+      P.counts[3] = (int)(free_first + taken);
+    }
+  }
+  const long long step = (long long)gridDim.x * STEP_THREADS * STEP_ROWS;
+  for (long long r0 = ((long long)blockIdx.x * STEP_THREADS + threadIdx.x) * STEP_ROWS; r0 < P.T; r0 += step) {
+    int slot[STEP_ROWS], pos[STEP_ROWS];
+    int s = (int)r0 < rows ? last_not_above(row_start, n, (int)r0) : n;
+    long long c = 0;
+    if (s < n) { c = P.cached[s]; c = c < 0 ? 0 : c; }
+#pragma unroll
+    for (int i = 0; i < STEP_ROWS; ++i) {
+      const int r = (int)r0 + i;
+      slot[i] = -1; pos[i] = 0;
+      if (r0 + i >= rows) continue;
+      if (row_start[s + 1] <= r) {               // the next sequence that has rows
+        do { ++s; } while (row_start[s + 1] <= r);
+        c = P.cached[s]; c = c < 0 ? 0 : c;
+      }
+      const long long p = c + (r - row_start[s]);
+      pos[i] = (int)(p < INT32_MAX ? p : INT32_MAX);
+      const long long page = p / bt, off = p - page * bt;
+      if (page >= P.table_pitch) continue;
+      const long long first = (c + bt - 1) / bt;
+      long long id;
+      if (page < first) {
+        id = P.table[s * P.table_pitch + page];
+      } else {
+        const long long k = need_start[s] + (page - first);
+        id = k < have ? P.free_list[free_first + k] : -1;
+        if (id < 0 || id >= P.n_pool_blocks) id = -1;
+        if (off == 0) P.table[s * P.table_pitch + page] = (int)id;
+      }
+      if (id >= 0 && id < P.n_pool_blocks) slot[i] = (int)(id * bt + off);
+    }
+    if (P.vec && r0 + STEP_ROWS <= P.T) {
+      *reinterpret_cast<int4 *>(P.slots + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+      *reinterpret_cast<int4 *>(P.positions + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < STEP_ROWS; ++i)
+        if (r0 + i < P.T) { P.slots[r0 + i] = slot[i]; P.positions[r0 + i] = pos[i]; }
+    }
+  }
+}
+
+// ---- the plan of the compacting copy --------------------------------------------------------------
+constexpr int PLAN_IDS = 8;                                   // consecutive blocks of the walk per thread
+constexpr int PLAN_CHUNK = STEP_THREADS * PLAN_IDS;           // blocks of the walk per workgroup
+enum { KV_PLAN_BAD_BLOCK = 1, KV_PLAN_BUFFER_FULL = 2, KV_PLAN_TABLE_FULL = 4, KV_PLAN_RUNS_FULL = 8 };
+
+struct KvPlanParams {
+  const int *table, *n_tokens, *n_new;
+  int *plan, *remap, *positions;
+  long long table_pitch, remap_pitch, n_pool_blocks, buffer_blocks, capacity;
+  int n_seqs, block_tokens, n_chunks;
+};
+
+// The walk goes through the sequences in table order and their blocks in logical order; block d of the
+// walk goes to block d of the buffer.  A block begins a run unless its physical id follows on that of
+// the block before it.  Workgroups 0 .. n_chunks - 1 write the runs of PLAN_CHUNK blocks each; the number
+// of runs before its chunk a workgroup counts by itself (one pass over the ids of the earlier chunks,
+// about a microsecond for every 8192 blocks, which is less than a second launch up to some 30000 blocks).
+// The other workgroups write the remapped table and the positions.
+__global__ __launch_bounds__(STEP_THREADS) void kv_plan_kernel(const KvPlanParams P) {
+  __shared__ int start[STEP_MAX_SEQS + 1];                    // first block of the walk of every sequence
+  __shared__ long long scratch64[STEP_THREADS / 64];
+  __shared__ int scratch[STEP_THREADS / 64];
+  const int n = P.n_seqs, bt = P.block_tokens, tid = threadIdx.x;
+  const long long most = P.remap && P.remap_pitch < P.table_pitch ? P.remap_pitch : P.table_pitch;
+  long long before = 0;
+  int flags = 0;
+  for (int s0 = 0; s0 < n; s0 += STEP_THREADS) {
+    const int s = s0 + tid;
+    long long nb = 0;
+    if (s < n) {
+      long long t = P.n_tokens[s], m = P.n_new ? P.n_new[s] : 0;
+      t = (t < 0 ? 0 : t) + (m < 0 ? 0 : m);
+      nb = (t + bt - 1) / bt;
+      if (nb > most) { nb = most; flags |= KV_PLAN_TABLE_FULL; }
+    }
+    long long total;
+    const long long end = before + block_scan(nb, scratch64, &total);
+    before += total;
+    if (s < n) start[s] = (int)(end - nb < P.buffer_blocks ? end - nb : P.buffer_blocks);
+  }
+  if (before > P.buffer_blocks) flags |= KV_PLAN_BUFFER_FULL;
+  const int nb = (int)(before < P.buffer_blocks ? before : P.buffer_blocks);
+  if (tid == 0) start[n] = nb;
+  __syncthreads();
+
+  if ((int)blockIdx.x < P.n_chunks) {
+    const int chunk = blockIdx.x, last_chunk = nb > 0 ? (nb - 1) / PLAN_CHUNK : 0;
+    if (chunk > last_chunk) return;
+    int runs = 0, last_head = 0;                              // of the chunks before
+    for (int c = 0; c <= chunk; ++c) {
+      const int d0 = c * PLAN_CHUNK + tid * PLAN_IDS;
+      // ids of the blocks d0 - 1 .. d0 + PLAN_IDS of the walk; -1: none, or outside the pool
+      int id[PLAN_IDS + 2];
+      const int from = d0 > 0 ? d0 - 1 : 0;
+      int s = from < nb ? last_not_above(start, n, from) : n;
+#pragma unroll
+      for (int i = 0; i < PLAN_IDS + 2; ++i) {
+        const int d = d0 - 1 + i;
+        id[i] = -1;
+        if (d < 0 || d >= nb) continue;
+        while (start[s + 1] <= d) ++s;
+        const int p = P.table[s * P.table_pitch + (d - start[s])];
+        id[i] = p >= 0 && p < P.n_pool_blocks ? p : -1;
+        if (id[i] < 0) flags |= KV_PLAN_BAD_BLOCK;
+      }
+      unsigned heads = 0;                                     // bit i: block d0 + i begins a run (i = PLAN_IDS: the one after mine)
+      int mine = 0, top = -1;
+#pragma unroll
+      for (int i = 0; i <= PLAN_IDS; ++i) {
+        const int d = d0 + i;
+        const bool head = d >= nb || id[i + 1] < 0 || id[i] < 0 || id[i + 1] != id[i] + 1;
+        if (head) heads |= 1u << i;
+        if (head && i < PLAN_IDS && d < nb) { ++mine; top = d; }
+      }
+      int total;
+      const int end = block_scan(mine, scratch, &total);
+      // the last head at or before my blocks: a running maximum over the threads, carried on the count of heads
+      // (heads ascend with the walk, so the maximum so far is that of the nearest thread before with any)
+      int carry = top;
+      const int lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(carry, o, 64);
+        if (lane >= o && u > carry) carry = u;
+      }
+      __syncthreads();
+      if (lane == 63) scratch[wave] = carry;
+      __syncthreads();
+      int wave_before = last_head, all = last_head;
+      for (int w = 0; w < STEP_THREADS / 64; ++w) {
+        const int u = scratch[w];
+        if (w < wave && u > wave_before) wave_before = u;
+        if (u > all) all = u;
+      }
+      int open = __shfl_up(carry, 1, 64);                      // head of the run that is open before my first block
+      if (lane == 0 || open < wave_before) open = wave_before;
+      if (c == chunk) {
+        int r = runs + end - mine - 1;                         // index of the run that is open
+#pragma unroll
+        for (int i = 0; i < PLAN_IDS; ++i) {
+          const int d = d0 + i;
+          if (d >= nb) break;
+          if (heads & (1u << i)) {
+            ++r; open = d;
+            if (r < P.capacity) { int *q = P.plan + KV_PLAN_HEADER + 3LL * r; q[0] = id[i + 1]; q[1] = d; }
+          }
+          if ((heads & (2u << i)) && r < P.capacity) P.plan[KV_PLAN_HEADER + 3LL * r + 2] = d + 1 - open;
+        }
+      }
+      runs += total;
+      last_head = all;
+    }
+    if (chunk == last_chunk) {                                 // this workgroup has seen every block
+      if (runs > P.capacity) flags |= KV_PLAN_RUNS_FULL;
+      int any = 0;
+#pragma unroll
+      for (int b = 1; b <= KV_PLAN_RUNS_FULL; b <<= 1) any |= __syncthreads_or(flags & b) ? b : 0;
+      if (tid == 0) {
+        P.plan[0] = any ? 0 : runs; P.plan[1] = any ? 0 : nb;
+        P.plan[2] = any; P.plan[3] = 0;
+      }
+      for (long long i = (runs < P.capacity ? runs : P.capacity) * 3LL + tid; i < 3 * P.capacity; i += STEP_THREADS) P.plan[KV_PLAN_HEADER + i] = 0;
+    }
+    return;
+  }
+
+  const long long worker = (long long)((int)blockIdx.x - P.n_chunks) * STEP_THREADS + tid;
+  const long long workers = (long long)((int)gridDim.x - P.n_chunks) * STEP_THREADS;
+  if (P.remap)
+    for (long long x = worker; x < n * P.remap_pitch; x += workers) {
+      const int s = (int)(x / P.remap_pitch);
+      const long long i = x - s * P.remap_pitch, d = start[s] + i;
+      int to = -1;
+      if (d < start[s + 1]) {
+        const int p = P.table[s * P.table_pitch + i];
+        if (p >= 0 && p < P.n_pool_blocks) to = (int)d;
+      }
+      P.remap[x] = to;
+    }
+  if (P.positions)
+    for (long long x = worker; x < P.buffer_blocks; x += workers) {
+      int base = -1;
+      if (x < nb) { const int s = last_not_above(start, n, (int)x); base = ((int)x - start[s]) * bt; }
+      for (int j = 0; j < bt; ++j) P.positions[x * bt + j] = base < 0 ? 0 : base + j;
+    }
+}
+
+// ---- drafted trees ------------------------------------------------------------------------------
+constexpr int TREE_THREADS = 256;
+constexpr int TREE_MAX_WORDS = 32;
+
+// LDS of tree_mask_kernel in bytes: the bits of 32 words rows (one word of padding per row), two lists of ancestors
+__host__ __device__ constexpr int tree_mask_lds(int words) { return 4 * (32 * words * (words + 1) + 2 * 32 * words); }
+
+// Row j of a sequence sees itself and its ancestors.  Pointer doubling in LDS: in round k every row has the
+// bits of its 2^k nearest ancestors and a pointer to the one 2^k above it; it takes over that row's bits and
+// that row's pointer.  ceil(log2(depth)) rounds instead of a walk of `depth` dependent steps.  A row may
+// read bits that their owner has already extended in the same round: those are ancestors too, and the pointers
+// are kept in two lists, so every round does what it has to.  The depth is the number of bits less one.
+__global__ __launch_bounds__(TREE_THREADS) void tree_mask_kernel(const int *parents, const int *row_start, const int *cached, int n_seqs, int T,
+                                                                 uint32_t *mask, int words, int *positions) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char tree_smem[];
+  uint32_t *bits = reinterpret_cast<uint32_t *>(tree_smem);    // [32 words][words + 1]
+  const int most = 32 * words, pitch = words + 1;
+  int *anc = reinterpret_cast<int *>(bits + most * pitch);     // [2][32 words]
+  for (int s = blockIdx.x; s < n_seqs; s += gridDim.x) {
+    int r0 = row_start[s], r1 = row_start[s + 1];
+    r0 = r0 < 0 ? 0 : r0; r1 = r1 > T ? T : r1;
+    if (r1 <= r0) continue;                                    // (the same in every thread)
+    const int rows = r1 - r0, n = rows < most ? rows : most;
+    int c = cached[s];
+    c = c < 0 ? 0 : c;
+    for (int j = threadIdx.x; j < n; j += TREE_THREADS) {
+      const int p = parents[r0 + j];
+      anc[j] = p >= 0 && p < j ? p : -1;
+    }
+    for (int x = threadIdx.x; x < n * words; x += TREE_THREADS) {
+      const int j = x / words, w = x - j * words;
+      bits[j * pitch + w] = j / 32 == w ? 1u << (j & 31) : 0u;
+    }
+    __syncthreads();
+    int *from = anc, *to = anc + most;
+    for (int span = 1; span < n; span *= 2) {                  // (an ancestor is at most n - 1 steps away)
+      int more = 0;
+      for (int x = threadIdx.x; x < n * words; x += TREE_THREADS) {
+        const int j = x / words, w = x - j * words, a = from[j];
+        if (a >= 0) bits[j * pitch + w] |= bits[a * pitch + w];
+      }
+      for (int j = threadIdx.x; j < n; j += TREE_THREADS) {
+        const int a = from[j], b = a >= 0 ? from[a] : -1;
+        to[j] = b;
+        more |= b >= 0;
+      }
+      if (!__syncthreads_or(more)) break;
+      int *t = from; from = to; to = t;
+    }
+    __syncthreads();
+    for (long long x = threadIdx.x; x < (long long)rows * words; x += TREE_THREADS) {
+      const int j = (int)(x / words), w = (int)(x - (long long)j * words);
+      mask[(long long)(r0 + j) * words + w] = j < n ? bits[j * pitch + w] : 0u;
+    }
+    if (positions)
+      for (int j = threadIdx.x; j < rows; j += TREE_THREADS) {
+        int depth = 0;
+        if (j < n) {
+          for (int w = 0; w < words; ++w) depth += __popc(bits[j * pitch + w]);
+          --depth;
+        }
+        const long long p = (long long)c + depth;
+        positions[r0 + j] = (int)(p < INT32_MAX ? p : INT32_MAX);
+      }
+    __syncthreads();                                           // (the next sequence writes the same LDS)
+  }
+}
+
+}  // namespace deinfer
