@@ -7,6 +7,7 @@
 
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "common.h"
 #include "host_common.h"
@@ -46,9 +47,9 @@ AttPlan att_plan(int64_t T, int64_t n_seqs, int64_t n_q, int64_t n_kv, int64_t h
   AttPlan p;
   p.dp = head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256;
   const int64_t per_head = ceil_div(T * (n_q / n_kv), n_seqs > 0 ? n_seqs : 1);      // rows of a sequence and key head, on average
-  p.rows = per_head <= 16 || p.dp == 256 ? 16 : 128;
+  p.rows = per_head <= 16 ? 16 : p.dp == 256 || per_head <= 128 ? 128 : 256;
   const int cus = device_cus();
-  p.shares = 2 * (int64_t)(cus > 0 ? cus : 256);
+  p.shares = (p.rows == 16 ? 2 : 1) * (int64_t)(cus > 0 ? cus : 256);
   p.joins = ATT_WS_HEADER;
   p.ml = p.joins + (size_t)round_up(p.shares * 16, 256);
   p.part = p.ml + (size_t)round_up(2 * p.shares * p.rows * 8, 256);
@@ -56,24 +57,32 @@ AttPlan att_plan(int64_t T, int64_t n_seqs, int64_t n_q, int64_t n_kv, int64_t h
   return p;
 }
 
+template <int DT, int DP, bool FULL, bool POW2, int RT>
+int launch_attention_tiles(const AttPlan &pl, const AttParams &P, hipStream_t s) {
+  using C = AttTile<DP>;
+  if (C::LDS > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(&tree_attention_tile_kernel<DT, DP, FULL, POW2, RT>),
+                                                hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS) != hipSuccess)
+    return fail(DEINFER_ERR_DEVICE, "tree attention: LDS size refused");
+  hipLaunchKernelGGL((tree_attention_tile_kernel<DT, DP, FULL, POW2, RT>), dim3((unsigned)pl.shares), dim3(C::THREADS), C::LDS, s, P);
+  if (int rc = check_launch("tree attention")) return rc;
+  hipLaunchKernelGGL((tree_attention_join_kernel<DT, DP, 128 * RT>), dim3((unsigned)pl.shares), dim3(JOIN_THREADS), 0, s, P);
+  return check_launch("tree attention");
+}
 template <int DT, int DP, bool FULL, bool POW2>
-void launch_attention(const AttPlan &pl, const AttParams &P, hipStream_t s) {
-  const dim3 grid((unsigned)pl.shares);
-  if constexpr (DP < 256) {
-    if (pl.rows == 128) {
-      hipLaunchKernelGGL((tree_attention_kernel<DT, DP, FULL, POW2, 4, 1, 2>), grid, dim3(ATT_THREADS), 0, s, P);
-      hipLaunchKernelGGL((tree_attention_join_kernel<DT, DP, 128>), grid, dim3(JOIN_THREADS), 0, s, P);
-      return;
-    }
-  }
-  hipLaunchKernelGGL((tree_attention_kernel<DT, DP, FULL, POW2, 1, 4, 1>), grid, dim3(ATT_THREADS), 0, s, P);
-  hipLaunchKernelGGL((tree_attention_join_kernel<DT, DP, 16>), grid, dim3(JOIN_THREADS), 0, s, P);
+int launch_attention(const AttPlan &pl, const AttParams &P, hipStream_t s) {
+  if (pl.rows == 128) return launch_attention_tiles<DT, DP, FULL, POW2, 1>(pl, P, s);
+  if constexpr (DP < 256)
+    if (pl.rows == 256) return launch_attention_tiles<DT, DP, FULL, POW2, 2>(pl, P, s);
+  hipLaunchKernelGGL((tree_attention_kernel<DT, DP, FULL, POW2, 1, 4, 1>), dim3((unsigned)pl.shares), dim3(ATT_THREADS), 0, s, P);
+  if (int rc = check_launch("tree attention")) return rc;
+  hipLaunchKernelGGL((tree_attention_join_kernel<DT, DP, 16>), dim3((unsigned)pl.shares), dim3(JOIN_THREADS), 0, s, P);
+  return check_launch("tree attention");
 }
 template <int DT, int DP>
-void launch_attention_of(const AttPlan &pl, const AttParams &P, hipStream_t s) {
-  if (P.block_shift < 4) launch_attention<DT, DP, false, false>(pl, P, s);
-  else if (P.head_dim == DP) launch_attention<DT, DP, true, true>(pl, P, s);
-  else launch_attention<DT, DP, false, true>(pl, P, s);
+int launch_attention_of(const AttPlan &pl, const AttParams &P, hipStream_t s) {
+  if (P.block_shift < 4) return launch_attention<DT, DP, false, false>(pl, P, s);
+  if (P.head_dim == DP) return launch_attention<DT, DP, true, true>(pl, P, s);
+  return launch_attention<DT, DP, false, true>(pl, P, s);
 }
 
 template <typename TE>
@@ -276,6 +285,7 @@ int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_he
   if (ldq < wq || ldo < wq || ldk < wk || ldv < wk) return fail(DEINFER_ERR_INVALID_ARG, "tree attention: a pitch is smaller than heads * head_dim");
   if (ldk > MAX_PITCH || ldv > MAX_PITCH) return fail(DEINFER_ERR_UNSUPPORTED, "tree attention: a pitch of the cache above 2^26 elements");
   if (T == 0 || n_seqs == 0) return DEINFER_OK;
+  if (table_pitch * block_tokens > INT32_MAX / 2) return fail(DEINFER_ERR_UNSUPPORTED, "tree attention: more than 2^30 tokens in a row of the block table");
   if (n_pool_blocks == 0 || table_pitch == 0) return fail(DEINFER_ERR_INVALID_ARG, "tree attention: an empty pool or block table");
   if (!q || !k_pool || !v_pool || !out || !row_start || !cached || !block_table) return fail(DEINFER_ERR_INVALID_ARG, "tree attention: a pointer is NULL");
   if (out == q) return fail(DEINFER_ERR_INVALID_ARG, "tree attention: out must not be q");
@@ -290,8 +300,8 @@ int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_he
   P.q = static_cast<const uint16_t *>(q); P.k = static_cast<const uint16_t *>(k_pool); P.v = static_cast<const uint16_t *>(v_pool);
   P.out = static_cast<uint16_t *>(out);
   P.row_start = row_start; P.cached = cached; P.table = block_table; P.mask = mask;
-  P.ldq = ldq; P.ldk = ldk; P.ldv = ldv; P.ldo = ldo; P.table_pitch = table_pitch; P.n_pool_blocks = n_pool_blocks;
-  P.most_keys = table_pitch * block_tokens;
+  P.ldq = ldq; P.ldk = (uint32_t)(2 * ldk); P.ldv = (uint32_t)(2 * ldv); P.ldo = ldo; P.table_pitch = (int)table_pitch; P.n_pool_blocks = (int)n_pool_blocks;
+  P.most_keys = (int)(table_pitch * block_tokens);
   P.T = (int)T; P.n_seqs = (int)n_seqs; P.n_kv = (int)n_kv_heads; P.group = (int)(n_q_heads / n_kv_heads); P.head_dim = (int)head_dim;
   P.block_tokens = (int)block_tokens; P.mask_words = (int)mask_words;
   P.block_shift = 0;
@@ -305,13 +315,12 @@ int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_he
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto by_dim = [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
-    if (pl.dp == 64) launch_attention_of<DT, 64>(pl, P, s);
-    else if (pl.dp == 128) launch_attention_of<DT, 128>(pl, P, s);
-    else launch_attention_of<DT, 256>(pl, P, s);
+    if (pl.dp == 64) return launch_attention_of<DT, 64>(pl, P, s);
+    if (pl.dp == 128) return launch_attention_of<DT, 128>(pl, P, s);
+    return launch_attention_of<DT, 256>(pl, P, s);
   };
-  if (dtype == DEINFER_F16) by_dim(std::integral_constant<int, DT_F16>{});
-  else by_dim(std::integral_constant<int, DT_BF16>{});
-  return check_launch("tree attention");
+  if (dtype == DEINFER_F16) return by_dim(std::integral_constant<int, DT_F16>{});
+  return by_dim(std::integral_constant<int, DT_BF16>{});
 }
 
 }  // extern "C"

@@ -35,7 +35,9 @@ struct AttParams {
   uint16_t *out;
   const int *row_start, *cached, *table;
   const uint32_t *mask;
-  long long ldq, ldk, ldv, ldo, table_pitch, n_pool_blocks, most_keys;     // most_keys: tokens that a row of the table can hold
+  long long ldq, ldo;
+  uint32_t ldk, ldv;                             // in bytes
+  int table_pitch, n_pool_blocks, most_keys;     // most_keys: tokens that a row of the table can hold, at most 2^30
   int T, n_seqs, n_kv, group, head_dim, block_tokens, block_shift, mask_words;
   float scale2;                                  // scale log2(e): the exponentials are powers of two
   int n_shares;
@@ -44,32 +46,124 @@ struct AttParams {
   int4 *joins;                                   // [n_shares] tile of rows whose first share this is and that others share (sequence, head, tile, shares)
 };
 
-struct AttSeq { int row0, n, ctx; long long keys; };             // first row, rows, cached tokens, keys in all
+struct AttSeq { int row0, n, ctx, keys; };       // first row, rows, cached tokens, keys in all
 __device__ __forceinline__ AttSeq att_seq(const AttParams &P, int s) {
   AttSeq q;
   int r0 = P.row_start[s], r1 = P.row_start[s + 1];
   r0 = r0 < 0 ? 0 : r0; r1 = r1 > P.T ? P.T : r1;
   q.row0 = r0; q.n = r1 > r0 ? r1 - r0 : 0;
   const int c = P.cached[s];
-  q.ctx = c < 0 ? 0 : c;
-  const long long keys = (long long)q.ctx + q.n;
-  q.keys = keys < P.most_keys ? keys : P.most_keys;
+  q.ctx = c < 0 ? 0 : c < P.most_keys ? c : P.most_keys;          // (what the table has no room for is not seen)
+  q.keys = q.n < P.most_keys - q.ctx ? q.ctx + q.n : P.most_keys;
   return q;
 }
-template <int ROWS, int UNIT> struct AttTiles {                   // units of one sequence
-  long long units; int tiles, per_tile;
-  __device__ __forceinline__ AttTiles(const AttSeq &q, int group, int n_kv) {
-    tiles = (int)(((long long)q.n * group + ROWS - 1) / ROWS);
-    per_tile = (int)((q.keys + UNIT - 1) / UNIT);
-    per_tile = per_tile < 1 ? 1 : per_tile;                       // (rows without any key are written too)
-    units = (long long)n_kv * tiles * per_tile;
-  }
-};
-
 // a value that is the same in every lane, in scalar registers
 __device__ __forceinline__ long long uniform(long long x) {
   return ((long long)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x);
 }
+// Keys that some row of a tile sees: all of the sequence's, or in a causal chunk none behind the tile's last token.
+template <int ROWS> __device__ __forceinline__ int att_tile_keys(const AttParams &P, const AttSeq &q, int tile) {
+  const int rows = q.n * P.group, end = (tile + 1) * ROWS < rows ? (tile + 1) * ROWS : rows;
+  const int causal = q.ctx + (end - 1) / P.group + 1;             // (at most 2^30 + 2^28)
+  return P.mask || causal > q.keys ? q.keys : causal;
+}
+template <int ROWS, int UNIT> __device__ __forceinline__ int att_tile_units(const AttParams &P, const AttSeq &q, int tile) {
+  const int u = (att_tile_keys<ROWS>(P, q, tile) + UNIT - 1) / UNIT;
+  return u < 1 ? 1 : u;                          // (rows without any key are written too)
+}
+// units of one key head of a sequence
+template <int ROWS, int UNIT> __device__ __forceinline__ long long att_head_units(const AttParams &P, const AttSeq &q) {
+  const int tiles = (q.n * P.group + ROWS - 1) / ROWS;
+  if (P.mask || tiles <= 1) return tiles ? (long long)tiles * att_tile_units<ROWS, UNIT>(P, q, tiles - 1) : 0;
+  long long u = 0;
+  for (int t = 0; t < tiles; ++t) u += att_tile_units<ROWS, UNIT>(P, q, t);
+  return u;
+}
+
+// A workgroup's run of units, tile after tile.  Everything is the same in all lanes.
+template <int ROWS, int UNIT, int THREADS> struct AttRun {
+  long long per_share, cur, end, base;           // base: first unit of the present tile
+  AttSeq seq;
+  int s, h, tile, per_tile;
+
+  // scan: THREADS / 64 values, found: 2 values of LDS.  False: nothing to do
+  __device__ __forceinline__ bool begin(const AttParams &P, int share, long long *scan, long long *found) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    auto units_of = [&](int x) -> long long { return x < P.n_seqs ? P.n_kv * att_head_units<ROWS, UNIT>(P, att_seq(P, x)) : 0; };
+    auto scan_units = [&](long long u, long long *total) {           // inclusive sum over the threads
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const long long w = __shfl_up(u, o, 64);
+        if (lane >= o) u += w;
+      }
+      __syncthreads();
+      if (lane == 63) scan[wave] = u;
+      __syncthreads();
+      long long all = 0, before = 0;
+      for (int w = 0; w < THREADS / 64; ++w) { if (w < wave) before += scan[w]; all += scan[w]; }
+      *total = all;
+      return u + before;
+    };
+    // (the last pass over up to THREADS sequences is kept: with no more of them there is one pass)
+    long long total = 0, mine = 0, mine_end = 0;
+    for (int s0 = 0; s0 < P.n_seqs; s0 += THREADS) {
+      long long t;
+      mine = units_of(s0 + tid);
+      mine_end = scan_units(mine, &t);
+      total += t;
+    }
+    total = uniform(total);
+    per_share = (total + P.n_shares - 1) / P.n_shares;
+    cur = per_share * share;
+    end = cur + per_share < total ? cur + per_share : total;
+    if (cur >= end) return false;
+    long long before = 0;
+    for (int s0 = 0; s0 < P.n_seqs; s0 += THREADS) {
+      long long t = total;
+      if (P.n_seqs > THREADS) {
+        mine = units_of(s0 + tid);
+        mine_end = scan_units(mine, &t);
+      }
+      const long long e = before + mine_end;
+      if (mine > 0 && e - mine <= cur && cur < e) { found[0] = s0 + tid; found[1] = e - mine; }
+      before += t;
+      if (before > cur) break;
+    }
+    __syncthreads();
+    s = __builtin_amdgcn_readfirstlane((int)found[0]);
+    base = uniform(found[1]);
+    seq = att_seq(P, s);
+    const long long per_head = uniform(att_head_units<ROWS, UNIT>(P, seq));
+    h = (int)((cur - base) / per_head);
+    base += h * per_head;
+    tile = 0;
+    per_tile = att_tile_units<ROWS, UNIT>(P, seq, 0);
+    while (cur >= base + per_tile) { base += per_tile; per_tile = att_tile_units<ROWS, UNIT>(P, seq, ++tile); }
+    return true;
+  }
+  // The present tile's units [from, to); then on to the next tile.
+  __device__ __forceinline__ int from() const { return (int)(cur - base); }
+  __device__ __forceinline__ int to() const { return end - base < per_tile ? (int)(end - base) : per_tile; }
+  __device__ __forceinline__ bool next(const AttParams &P) {
+    cur = base + to();
+    if (cur >= end) return false;
+    base += per_tile;
+    if ((tile + 1) * ROWS < seq.n * P.group) {
+      ++tile;
+    } else {
+      tile = 0;
+      if (++h == P.n_kv) {
+        h = 0;
+        do { seq = att_seq(P, ++s); } while (seq.n == 0 && s + 1 < P.n_seqs);
+      }
+    }
+    per_tile = att_tile_units<ROWS, UNIT>(P, seq, tile);
+    return true;
+  }
+  // shares that have units of the present tile
+  __device__ __forceinline__ int sharers() const { return (int)((base + per_tile - 1) / per_share - base / per_share + 1); }
+};
+
 __device__ __forceinline__ float att_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 // the larger (the sum) of the four quarters of the wave, in every lane
 __device__ __forceinline__ float quarters_max(float x) {
@@ -79,6 +173,22 @@ __device__ __forceinline__ float quarters_max(float x) {
 __device__ __forceinline__ float quarters_sum(float x) {
   x += __shfl_xor(x, 16, 64);
   return x + __shfl_xor(x, 32, 64);
+}
+
+// Bits of the 32 keys from k0 on that row `token` of the sequence sees among the drafted ones (all ones for cached keys).
+__device__ __forceinline__ uint32_t att_window(const AttParams &P, const AttSeq &q, int k0, int token, bool row) {
+  if (!P.mask) {
+    const int n = q.ctx + token + 1 - k0;
+    return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
+  }
+  const int e = k0 - q.ctx;                      // first of the 32 as index among the step's own tokens
+  if (e <= -32) return 0xffffffffu;
+  const uint32_t *mw = P.mask + (long long)(q.row0 + token) * P.mask_words;
+  auto word = [&](int i) -> uint32_t { return row && i < P.mask_words ? mw[i] : 0u; };
+  if (e < 0) return (word(0) << -e) | ((1u << -e) - 1u);
+  uint32_t w = word(e >> 5) >> (e & 31);
+  if (e & 31) w |= word((e >> 5) + 1) << (32 - (e & 31));
+  return w;
 }
 
 // 16-bit elements of a word that are infinite or NaN
@@ -110,60 +220,12 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
   const int D = FULL ? DP : P.head_dim;
   const int share = run_tile_of(blockIdx.x, P.n_shares);
 
-  // ---- my run of units
-  auto units_of = [&](int s) -> long long {
-    if (s >= P.n_seqs) return 0;
-    return AttTiles<ROWS, UNIT>(att_seq(P, s), P.group, P.n_kv).units;
-  };
-  auto scan_units = [&](long long u, long long *total) {           // inclusive sum over the threads
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const long long w = __shfl_up(u, o, 64);
-      if (lane >= o) u += w;
-    }
-    __syncthreads();
-    if (lane == 63) scan[wave] = u;
-    __syncthreads();
-    long long all = 0, before = 0;
-    for (int w = 0; w < ATT_THREADS / 64; ++w) { if (w < wave) before += scan[w]; all += scan[w]; }
-    *total = all;
-    return u + before;
-  };
-  long long total = 0;
-  for (int s0 = 0; s0 < P.n_seqs; s0 += ATT_THREADS) {
-    long long t;
-    scan_units(units_of(s0 + tid), &t);
-    total += t;
-  }
-  total = uniform(total);
-  const long long per_share = (total + P.n_shares - 1) / P.n_shares;
-  long long cur = per_share * share;
-  const long long end = cur + per_share < total ? cur + per_share : total;
+  AttRun<ROWS, UNIT, ATT_THREADS> run;
   if (tid == 0) P.joins[share] = make_int4(-1, 0, 0, 0);
-  if (cur >= end) return;                                          // (the same in every thread)
-  {
-    long long base = 0;
-    for (int s0 = 0; s0 < P.n_seqs; s0 += ATT_THREADS) {
-      long long t;
-      const long long u = units_of(s0 + tid), e = base + scan_units(u, &t);
-      if (u > 0 && e - u <= cur && cur < e) { found[0] = s0 + tid; found[1] = e - u; }
-      base += t;
-      if (base > cur) break;
-    }
-    __syncthreads();
-  }
-  int s = __builtin_amdgcn_readfirstlane((int)found[0]);
-  long long seq_base = uniform(found[1]);
-
-  while (cur < end) {
-    const AttSeq seq = att_seq(P, s);
-    const AttTiles<ROWS, UNIT> ti(seq, P.group, P.n_kv);
-    if (cur >= seq_base + ti.units) { seq_base += ti.units; ++s; continue; }
-    const long long in_seq = cur - seq_base;
-    const int h = (int)(in_seq / ((long long)ti.tiles * ti.per_tile));
-    const long long in_head = in_seq - (long long)h * ti.tiles * ti.per_tile;
-    const int tile = (int)(in_head / ti.per_tile), u0 = (int)(in_head - (long long)tile * ti.per_tile);
-    const int u1 = end - cur < ti.per_tile - u0 ? u0 + (int)(end - cur) : ti.per_tile;
+  if (!run.begin(P, share, scan, found)) return;                   // (the same in every thread)
+  do {
+    const AttSeq seq = run.seq;
+    const int s = run.s, h = run.h, tile = run.tile, u0 = run.from(), u1 = run.to();
 
     // ---- the rows
     const int n_rows = seq.n * P.group - tile * ROWS < ROWS ? seq.n * P.group - tile * ROWS : ROWS;   // of this tile
@@ -189,67 +251,66 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
 #pragma unroll
       for (int f = 0; f < NF; ++f) o[rt][f] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    const int first_token = tile * ROWS / P.group, last_token = (tile * ROWS + n_rows - 1) / P.group;
-    // keys that some row may see (a causal tile needs none behind its last token), and keys that every row sees
-    long long keys_end = P.mask ? seq.keys : (long long)seq.ctx + last_token + 1;
-    keys_end = keys_end < seq.keys ? keys_end : seq.keys;
-    const long long keys_all = P.mask ? seq.ctx : (long long)seq.ctx + first_token + 1;
+    // keys that some row may see, and keys that every row sees
+    const int keys_end = att_tile_keys<ROWS>(P, seq, tile);
+    const int keys_all = P.mask ? seq.ctx : seq.ctx + tile * ROWS / P.group + 1;
 
-    const int *table = P.table + s * P.table_pitch;
-    const int klane = col * (int)P.ldk + quarter * 8, vlane = quarter * 4 * (int)P.ldv + col * VE;
-    for (long long k0 = (long long)u0 * UNIT + wk * ATT_KEYS; k0 < (long long)u1 * UNIT && k0 < keys_end; k0 += UNIT) {
+    const int *table = P.table + (long long)s * P.table_pitch;
+    const char *kh = reinterpret_cast<const char *>(P.k + (long long)h * D), *vh = reinterpret_cast<const char *>(P.v + (long long)h * D);
+    const uint32_t klane = col * P.ldk + quarter * 16, vlane = quarter * 4 * P.ldv + col * VE * 2;
+    const int k_last = u1 * UNIT < keys_end ? u1 * UNIT : keys_end;
+    for (int k0 = u0 * UNIT + wk * ATT_KEYS; k0 < k_last; k0 += UNIT) {
       // ---- where the 32 keys are; `live`: those that exist
-      uint32_t live = keys_end - k0 >= 32 ? 0xffffffffu : (1u << (int)(keys_end - k0)) - 1u;
-      const uint16_t *kp[2], *vp[2];             // POW2: rows of the two halves' first keys
-      long long slot = 0;                        // otherwise: row of the key k0 + lane % 32
+      uint32_t live = keys_end - k0 >= 32 ? 0xffffffffu : (1u << (keys_end - k0)) - 1u;
+      const char *kp[2], *vp[2];                 // POW2: rows of the two halves' first keys
+      int slot = 0;                              // otherwise: row of the key k0 + lane % 32
       if constexpr (POW2) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const long long kk = k0 + 16 * u;
+          const int kk = k0 + 16 * u;
           int id = -1;
           if (kk < keys_end) id = table[kk >> P.block_shift];
           const bool ok = id >= 0 && id < P.n_pool_blocks;
           if (!ok) live &= ~(0xffffu << (16 * u));
-          const long long row = ok ? ((long long)id << P.block_shift) + (kk & (P.block_tokens - 1)) : 0;
-          kp[u] = P.k + row * P.ldk + (long long)h * D;
-          vp[u] = P.v + row * P.ldv + (long long)h * D;
+          const uint64_t row = ok ? (uint32_t)((id << P.block_shift) + (kk & (P.block_tokens - 1))) : 0u;
+          kp[u] = kh + row * P.ldk;
+          vp[u] = vh + row * P.ldv;
         }
       } else {
-        const long long kk = k0 + (lane & 31);
+        const int kk = k0 + (lane & 31);
         bool ok = false;
         if (kk < keys_end) {
-          const long long page = kk / P.block_tokens;
-          const int id = table[page];
+          const int page = kk / P.block_tokens, id = table[page];
           ok = id >= 0 && id < P.n_pool_blocks;
-          if (ok) slot = (long long)id * P.block_tokens + (kk - page * P.block_tokens);
+          if (ok) slot = id * P.block_tokens + (kk - page * P.block_tokens);
         }
         live &= (uint32_t)__ballot(ok);
       }
       u32x4_t kf[2][KS];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const uint16_t *kr;
+        const char *kr;
         if constexpr (POW2) kr = kp[u] + klane;
-        else kr = P.k + __shfl(slot, 16 * u + col, 64) * P.ldk + (long long)h * D + quarter * 8;
+        else kr = kh + (uint64_t)(uint32_t)__shfl(slot, 16 * u + col, 64) * P.ldk + quarter * 16;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           kf[u][ks] = u32x4_t{0u, 0u, 0u, 0u};
-          if (FULL || ks * 32 + quarter * 8 < D) kf[u][ks] = *reinterpret_cast<const u32x4_t *>(kr + ks * 32);
+          if (FULL || ks * 32 + quarter * 8 < D) kf[u][ks] = *reinterpret_cast<const u32x4_t *>(kr + ks * 64);
         }
       }
       uint32_t vw[NC][8][VW];                    // [piece][key 4 u + i of the lane][word]
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
-        const uint16_t *vr;
-        if constexpr (POW2) vr = vp[x / 4] + (vlane + (x % 4) * (int)P.ldv);
-        else vr = P.v + __shfl(slot, 16 * (x / 4) + 4 * quarter + x % 4, 64) * P.ldv + (long long)h * D + col * VE;
+        const char *vr;
+        if constexpr (POW2) vr = vp[x / 4] + (x % 4) * P.ldv + vlane;
+        else vr = vh + (uint64_t)(uint32_t)__shfl(slot, 16 * (x / 4) + 4 * quarter + x % 4, 64) * P.ldv + col * VE * 2;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
 #pragma unroll
           for (int w = 0; w < VW; ++w) vw[c][x][w] = 0u;
           if (FULL || c * 16 * VE + col * VE < D) {
             if constexpr (VE == 8) {
-              const u32x4_t t = *reinterpret_cast<const u32x4_t *>(vr + c * 128);
+              const u32x4_t t = *reinterpret_cast<const u32x4_t *>(vr + c * 256);
 #pragma unroll
               for (int w = 0; w < 4; ++w) vw[c][x][w] = t[w];
             } else {
@@ -278,23 +339,7 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
         odd_v = __any(odd_v);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-          uint32_t w = 0xffffffffu;
-          if (!P.mask) {
-            const long long n = (long long)seq.ctx + token[rt] + 1 - k0;
-            w = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << (int)n) - 1u;
-          } else if (k0 + 32 > seq.ctx) {
-            const long long e = k0 - seq.ctx;    // first key of the 32 as index among the step's tokens; > -32
-            const uint32_t *mw = P.mask + (long long)(seq.row0 + token[rt]) * P.mask_words;
-            const bool row = (wr * RT + rt) * 16 + col < n_rows;
-            auto word = [&](long long i) -> uint32_t { return row && i < P.mask_words ? mw[i] : 0u; };
-            if (e < 0) {
-              w = (word(0) << (int)-e) | ((1u << (int)-e) - 1u);
-            } else {
-              const int sh = (int)(e & 31);
-              w = word(e >> 5) >> sh;
-              if (sh) w |= word((e >> 5) + 1) << (32 - sh);
-            }
-          }
+          const uint32_t w = att_window(P, seq, k0, token[rt], (wr * RT + rt) * 16 + col < n_rows);
           sees[rt] = w & live;
         }
       }
@@ -361,8 +406,8 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
             const float pk = __shfl(mine, ((kk >> 2) & 3) * 16 + col, 64);
             const bool see = (sees[rt] >> kk) & 1u;
             const uint16_t *vr;
-            if constexpr (POW2) vr = (kk < 16 ? vp[0] : vp[1]) + (kk & 15) * P.ldv;
-            else vr = P.v + __shfl(slot, kk, 64) * P.ldv + (long long)h * D;
+            if constexpr (POW2) vr = reinterpret_cast<const uint16_t *>((kk < 16 ? vp[0] : vp[1]) + (kk & 15) * P.ldv);
+            else vr = reinterpret_cast<const uint16_t *>(vh + (uint64_t)(uint32_t)__shfl(slot, kk, 64) * P.ldv);
 #pragma unroll
             for (int f = 0; f < NF; ++f)
 #pragma unroll
@@ -376,7 +421,7 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
     }
 
     // ---- out: to the rows, where this workgroup had all their keys, else to the workspace
-    const bool whole = u0 == 0 && u1 == ti.per_tile;
+    const bool whole = u0 == 0 && u1 == run.per_tile;
     const long long which = 2LL * share + (u0 == 0 ? 1 : 0);        // (a tile that begins here is the last of the run, one that does not the first)
     auto store_row = [&](int r, int d, const float *x, float mm, float ll) {      // VE features from d of row r of the tile; ll: their sum
       if (whole) {
@@ -446,12 +491,424 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
         }
       }
     }
-    if (!whole && u0 == 0 && tid == 0) {
-      const long long first = cur, last = cur + ti.per_tile - 1;
-      P.joins[share] = make_int4(s, h, tile, (int)(last / per_share - first / per_share + 1));
+    if (!whole && u0 == 0 && tid == 0) P.joins[share] = make_int4(s, h, tile, run.sharers());
+  } while (run.next(P));
+}
+
+// The same work where a sequence and key head has more than a few rows: eight wavefronts with RT tiles of 16 rows each
+// share the keys, STAGE at a time, through LDS, a ring of four stages.  The rows of K and V come straight from
+// memory into the ring, three stages ahead of their use (no registers, no waiting; one barrier per stage).  Rows
+// lie in LDS as they do in memory but for their 16-byte pieces, which are XORed with the row's number: sixteen rows at one
+// place (an operand of K), and four neighbouring features of sixteen rows (the transposing read that makes V^T's
+// operand), then cover all banks.  V needs no permutes here, and its features keep their order: block f of the
+// output is 16 f .. 16 f + 15.
+//
+// Per stage a wavefront has 64 RT / 2 matrix instructions and 16 RT exponentials per lane, which take about as long;
+// so the scores of the stage after are multiplied while those of this one are turned into probabilities, and
+// the rest of the softmax is kept off the vector unit:
+//  - the sum l is a product too, P with a row of ones (and so the sum of the rounded probabilities);
+//  - there is no maximum in the common case.  The reference m of a row is set so that the largest probability is 2^-REF; a
+//    later score may pass it, and only if a probability is then too large for the type's comfort (att_large) are
+//    the maximum, the rescaling of O and l and the probabilities formed (again, from the keys, which are still in LDS).
+//    Precision is relative in both types: bf16 takes REF = 16 and lets a probability grow to 2; fp16, whose smallest
+//    normal number is 2^-14, takes 0 and lets one grow to 2^15.
+template <int DP> struct AttTile {
+  static constexpr int STAGE = DP == 256 ? 32 : 64;
+  static constexpr int THREADS = 512, RING = 4, IDS = 1024, LDS = RING * 2 * STAGE * DP * 2 + IDS * 4;
+};
+__device__ const u32x4_t att_zeros = {0u, 0u, 0u, 0u};
+
+// Whether a probability needs a new reference: a running value over packed pairs, and its test.  bf16: one of 2 or more
+// has a bit of its own.  fp16: one of 2^15 or more, found behind the pairs' maximum.  Infinity and NaN count in both.
+template <int DT> __device__ __forceinline__ uint32_t att_larger(uint32_t any, uint32_t lo, uint32_t hi) {
+  if constexpr (DT == DT_F16) {
+    typedef unsigned short pair_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_elementwise_max(__builtin_bit_cast(pair_t, lo), __builtin_bit_cast(pair_t, hi)), __builtin_bit_cast(pair_t, any)));
+  } else return any | lo | hi;
+}
+template <int DT> __device__ __forceinline__ bool att_large(uint32_t any) {
+  if constexpr (DT == DT_F16) return ((any | (any + 0x08000800u)) & 0x80008000u) != 0;
+  else return (any & 0x40004000u) != 0;
+}
+
+// 16 bytes per lane from memory into LDS, to `to` (the same in every lane) + 16 lane.  In asm (nothing but LDS is written; the
+// waits are written out where they belong) because with the compiler's own such load in flight every wait for an
+// operand from LDS becomes one for all of them.
+__device__ __forceinline__ uint32_t lds_at(void *to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_readfirstlane((uint32_t)(__attribute__((address_space(3))) unsigned char *)to);
+#else
+  (void)to; return 0;
+#endif
+}
+__device__ __forceinline__ void load_to_lds(const void *from, void *to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_at(to)), "v"(from) : "memory", "m0");
+#else
+  (void)from; (void)to;
+#endif
+}
+// the same with an address that is the wavefront's and a lane's offset
+__device__ __forceinline__ void load_to_lds(const void *from, uint32_t offset, void *to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_at(to)), "v"(offset), "s"(from) : "memory", "m0");
+#else
+  (void)from; (void)offset; (void)to;
+#endif
+}
+// Lanes 4 r + c of sixteen address 8 bytes (columns 4 c .. 4 c + 3) of row r < 4; lane j gets column j of the four rows.
+__device__ __forceinline__ uint2 read_transposed(const unsigned char *p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef short s16x4_t __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)p));
+#else
+  (void)p;
+  return make_uint2(0u, 0u);
+#endif
+}
+
+template <int DT, int DP, bool FULL, bool POW2, int RT>
+__global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttParams P) {
+  using C = AttTile<DP>;
+  constexpr int ROWS = 128 * RT, STAGE = C::STAGE, THREADS = C::THREADS;
+  constexpr int KS = DP / 32, NF = DP / 16;      // k steps of the first product, feature blocks of the second
+  constexpr int CH = DP / 8, ROWB = DP * 2;      // 16-byte pieces and bytes of a row in LDS
+  constexpr int SW = (CH < 16 ? CH : 16) - 1;
+  constexpr int WROWS = STAGE / 8;               // rows of K (of V) that a wavefront loads of a stage
+  constexpr int RPI = 64 / CH, NL = WROWS / RPI; // rows of one load instruction, load instructions
+  constexpr int HALVES = STAGE / 32;
+  constexpr int BUF = STAGE * ROWB;              // bytes of K (of V) of a stage
+  constexpr float REF = DT == DT_F16 ? 0.0f : 16.0f;
+  constexpr uint32_t ONES = DT == DT_F16 ? 0x3c003c00u : 0x3f803f80u;
+  static_assert(NL * RPI == WROWS, "whole load instructions");
+  extern __shared__ __attribute__((aligned(16))) unsigned char att_smem[];       // [RING][K, V][STAGE][ROWB], [IDS]
+  int *ids = reinterpret_cast<int *>(att_smem + C::RING * 2 * BUF);              // the sequence's blocks from page0 on
+  __shared__ long long scan[THREADS / 64];
+  __shared__ long long found[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, quarter = lane >> 4;
+  const int D = FULL ? DP : P.head_dim;
+  const int share = run_tile_of(blockIdx.x, P.n_shares);
+  AttRun<ROWS, STAGE, THREADS> run;
+  if (tid == 0) P.joins[share] = make_int4(-1, 0, 0, 0);
+  if (!run.begin(P, share, scan, found)) return;                   // (the same in every thread)
+
+  // byte offset of this lane's operand of K in 16 rows, for the first k step; for step ks its bits of 64 ks are the other way
+  const int kbase = col * ROWB + ((quarter ^ (col & SW)) * 16);
+  const int vrow = 4 * quarter + (col >> 2);     // row of 16 that this lane addresses in a transposing read of V
+  const int vswz = (((col & 3) >> 1) ^ (vrow & SW)) * 16, vbase = vrow * ROWB + (col & 1) * 8;
+  const u32x4_t ones = {ONES, ONES, ONES, ONES};
+
+  do {
+    const AttSeq seq = run.seq;
+    const int s = run.s, h = run.h, tile = run.tile, u0 = run.from(), u1 = run.to();
+    const int n_rows = seq.n * P.group - tile * ROWS < ROWS ? seq.n * P.group - tile * ROWS : ROWS;   // of this tile
+    const bool mine = wave * RT * 16 < n_rows;   // this wavefront has rows
+    u32x4_t qf[RT][KS];
+    int token[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int r = (wave * RT + rt) * 16 + col, gr = tile * ROWS + r;
+      const int j = gr / P.group, hh = gr - j * P.group;
+      token[rt] = j;
+      const uint16_t *qp = P.q + (long long)(seq.row0 + j) * P.ldq + (long long)(h * P.group + hh) * D + quarter * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        qf[rt][ks] = u32x4_t{0u, 0u, 0u, 0u};
+        if (r < n_rows && (FULL || ks * 32 + quarter * 8 < D)) qf[rt][ks] = *reinterpret_cast<const u32x4_t *>(qp + ks * 32);
+      }
     }
-    cur += u1 - u0;
-  }
+    f32x4_t o[RT][NF], l[RT];
+    float m[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      m[rt] = -__builtin_inff(); l[rt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int f = 0; f < NF; ++f) o[rt][f] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    const int keys_end = att_tile_keys<ROWS>(P, seq, tile);                   // at least 1
+    const int keys_all = P.mask ? seq.ctx : seq.ctx + tile * ROWS / P.group + 1;
+    const int *table = P.table + (long long)s * P.table_pitch;
+    const char *kh = reinterpret_cast<const char *>(P.k + (long long)h * D), *vh = reinterpret_cast<const char *>(P.v + (long long)h * D);
+
+    // The blocks of the keys to be loaded are read from the table ahead, IDS at a time, into LDS: a wait for a list in
+    // memory would be one for the rows in flight too.  Every wavefront calls this, between barriers.
+    int page0 = 0;
+    auto fetch_ids = [&](int k0) {
+      page0 = k0 / P.block_tokens;
+      const int last = (keys_end - 1) / P.block_tokens;
+      for (int x = tid; x < C::IDS; x += THREADS) ids[x] = table[page0 + x < last ? page0 + x : last];
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    };
+    // The wavefront's rows of K and of V of the stage of keys from k0 on into place b of the ring: 2 NL load instructions,
+    // whatever keys there are, so that the waits below can count them.  Keys that do not exist are rows of zeros.
+    // Returns the keys that exist.
+    auto issue = [&](int b, int k0) -> uint64_t {
+      unsigned char *kb = att_smem + b * 2 * BUF + wave * WROWS * ROWB, *vb = kb + BUF;
+      const int kk = k0 + (lane & (STAGE - 1)), ke = kk < keys_end ? kk : keys_end - 1;
+      const int page = POW2 ? ke >> P.block_shift : ke / P.block_tokens, off = POW2 ? ke & (P.block_tokens - 1) : ke - page * P.block_tokens;
+      const int id = ids[page > page0 ? page - page0 : 0];         // (behind the last stage nothing is read ahead)
+      const bool ok = kk < keys_end && id >= 0 && id < P.n_pool_blocks;
+      uint64_t live = __ballot(ok);
+      if constexpr (STAGE == 32) live &= 0xffffffffull;
+      const int slot = ok ? (POW2 ? (id << P.block_shift) + off : id * P.block_tokens + off) : 0;
+      const uint32_t here = (uint32_t)(live >> (WROWS * wave)) & ((1u << WROWS) - 1u);
+      const uint64_t row0 = (uint32_t)__builtin_amdgcn_readlane(slot, WROWS * wave);
+      const char *k0p = kh + row0 * P.ldk, *v0p = vh + row0 * P.ldv;
+      int ln = lane;
+      asm volatile("" : "+v"(ln));               // (the few instructions anew each time: kept through the loop they cost registers)
+      const int lrow = ln / CH, lpos = ln % CH;
+      auto load = [&](int i, bool all) {
+        // row lrow + RPI i of the wavefront's, row (WROWS wave + that) of the stage: its piece at place lpos
+        const int r = lrow + RPI * i;
+        const uint32_t piece = (uint32_t)(lpos ^ ((WROWS * wave + r) & SW));
+        const char *kr, *vr;
+        if constexpr (POW2) {
+          if (all) {
+            load_to_lds(k0p, r * P.ldk + piece * 16, kb + i * 1024);
+            load_to_lds(v0p, r * P.ldv + piece * 16, vb + i * 1024);
+            return;
+          }
+          kr = k0p + (r * P.ldk + piece * 16);
+          vr = v0p + (r * P.ldv + piece * 16);
+        } else {
+          const uint64_t row = (uint32_t)__shfl(slot, WROWS * wave + r, 64);
+          kr = kh + row * P.ldk + piece * 16;
+          vr = vh + row * P.ldv + piece * 16;
+        }
+        if (!all) {
+          const bool there = ((here >> r) & 1u) && (FULL || (int)piece * 8 < D);
+          kr = there ? kr : reinterpret_cast<const char *>(&att_zeros);
+          vr = there ? vr : reinterpret_cast<const char *>(&att_zeros);
+        }
+        load_to_lds(kr, kb + i * 1024);
+        load_to_lds(vr, vb + i * 1024);
+      };
+      if (FULL && here == (1u << WROWS) - 1u) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) load(i, true);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) load(i, false);
+      }
+      return live;
+    };
+    // operands of the keys 16 u .. 16 u + 15 of the stage at kb (kx: kbase), and their scores
+    auto read_k = [&](const unsigned char *kb, int kx, u32x4_t (&kf)[KS], int u) {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) kf[ks] = *reinterpret_cast<const u32x4_t *>(kb + u * 16 * ROWB + (kx ^ (ks * 64)));
+    };
+    auto scores = [&](const u32x4_t (&kf)[KS], f32x4_t (&x)[RT][2], int u) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) x[rt][u] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) x[rt][u] = mfma16<DT>(kf[ks], qf[rt][ks], x[rt][u]);
+    };
+
+    const int k_first = u0 * STAGE, k_last = u1 * STAGE < keys_end ? u1 * STAGE : keys_end;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();                // (the tile before has been read, and its last loads have landed)
+    asm volatile("" ::: "memory");
+    fetch_ids(k_first);
+    uint64_t live0 = issue(0, k_first), live1 = issue(1, k_first + STAGE), live2 = issue(2, k_first + 2 * STAGE);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * NL) : "memory");
+    __builtin_amdgcn_s_barrier();                // stage 0 has landed
+    asm volatile("" ::: "memory");
+    f32x4_t sc[RT][2];                           // scores of the next 32 keys
+    if (mine) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        u32x4_t kf[KS];
+        read_k(att_smem, kbase, kf, u);
+        scores(kf, sc, u);
+      }
+    }
+    int b = 0;
+    for (int k0 = k_first; k0 < k_last; k0 += STAGE, b = (b + 1) & 3) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * NL) : "memory");      // my rows of the next stage have landed
+      __builtin_amdgcn_s_barrier();                                                  // everybody's have; the stage before has been read
+      asm volatile("" ::: "memory");
+      // (ids of the stage's last key; three stages lie within IDS from the first)
+      const int ahead = k0 + 4 * STAGE - 1 < keys_end ? k0 + 4 * STAGE - 1 : keys_end - 1;
+      if ((POW2 ? ahead >> P.block_shift : ahead / P.block_tokens) >= page0 + C::IDS) fetch_ids(k0 + 3 * STAGE);
+      const uint64_t live3 = issue((b + 3) & 3, k0 + 3 * STAGE);
+      const unsigned char *kb = att_smem + b * 2 * BUF, *vb = kb + BUF, *kb_next = att_smem + ((b + 1) & 3) * 2 * BUF;
+      const uint64_t now = live0;
+      live0 = live1; live1 = live2; live2 = live3;
+      const bool masked = now != (STAGE == 64 ? ~0ull : 0xffffffffull) || k0 + STAGE > keys_all;
+      if (!mine) continue;
+      bool odd_v = false;
+      if (masked) {                              // is there a value that is infinite or NaN?
+#pragma unroll 1
+        for (int x = 0; x < BUF / 1024; ++x) {
+          const u32x4_t v = *reinterpret_cast<const u32x4_t *>(vb + x * 1024 + lane * 16);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) odd_v |= not_finite<DT>(v[w]);
+        }
+        odd_v = __any(odd_v);
+      }
+#pragma unroll
+      for (int c = 0; c < HALVES; ++c) {         // 32 keys
+        int kx = kbase, vx = vbase, vz = vswz, q4 = 4 * quarter;
+        asm volatile("" : "+v"(kx), "+v"(vx), "+v"(vz), "+v"(q4));      // (what is made of these is not kept through the loop)
+        const unsigned char *kn = c + 1 < HALVES ? kb + (c + 1) * 32 * ROWB : kb_next;      // the 32 keys after these
+        // Operands are read from LDS one group of matrix instructions ahead, which the barriers for the scheduler keep that
+        // way: left to itself it reads each right before its use.
+        u32x4_t kf[2][KS];
+        read_k(kn, kx, kf[0], 0);
+        uint32_t sees[RT];
+        auto hide = [&](f32x4_t (&x)[RT][2]) {
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (!((sees[rt] >> (16 * u + q4 + i)) & 1u)) x[rt][u][i] = -__builtin_inff();
+        };
+        if (masked) {
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            int t = token[rt];
+            asm volatile("" : "+v"(t));
+            sees[rt] = att_window(P, seq, k0 + 32 * c, t, (wave * RT + rt) * 16 + col < n_rows) & (uint32_t)(now >> (32 * c));
+          }
+          hide(sc);
+        }
+        // ---- probabilities of these keys (rounded to the type: off by at most half a step, which is what the
+        // output's own rounding is off by), beside the scores of the next
+        u32x4_t pf[RT];
+        uint32_t any = 0;
+        auto probabilities = [&](const f32x4_t (&x)[RT][2], int u) {
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            // (a row that has seen no key yet: any score but minus infinity then makes an infinity)
+            const float ref = m[rt] == -__builtin_inff() ? 1.0e30f : -m[rt];
+            float p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = att_exp2(fmaf(x[rt][u][i], P.scale2, ref));
+            const uint32_t lo = pack2<DT>(p[0], p[1]), hi = pack2<DT>(p[2], p[3]);
+            pf[rt][2 * u] = lo; pf[rt][2 * u + 1] = hi;
+            any = att_larger<DT>(any, lo, hi);
+          }
+        };
+        probabilities(sc, 0);
+        read_k(kn, kx, kf[1], 1);
+        __builtin_amdgcn_sched_barrier(0);
+        scores(kf[0], sc, 0);
+        probabilities(sc, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        scores(kf[1], sc, 1);
+        if (__any(att_large<DT>(any))) {
+          f32x4_t x[RT][2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            u32x4_t kr[KS];
+            read_k(kb, kx, kr, 2 * c + u);
+            scores(kr, x, u);
+          }
+          if (masked) hide(x);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            float top = x[rt][0][0];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) top = fmaxf(top, x[rt][u][i]);
+            const float m_new = fmaxf(m[rt], quarters_max(top) * P.scale2 + REF);
+            const float a = m[rt] == -__builtin_inff() ? 0.0f : att_exp2(m[rt] - m_new);
+            m[rt] = m_new;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) l[rt][i] *= a;
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[rt][f][i] *= a;
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u) probabilities(x, u);
+        }
+        if (!odd_v) {
+          uint2 va[2][2];
+          auto read_v = [&](uint2 (&v)[2], int f) {
+            const unsigned char *vp = vb + 32 * c * ROWB + vx + ((f * 32) ^ vz);
+            v[0] = read_transposed(vp); v[1] = read_transposed(vp + 16 * ROWB);
+          };
+          read_v(va[0], 0);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) l[rt] = mfma16<DT>(ones, pf[rt], l[rt]);
+#pragma unroll
+          for (int f = 0; f < NF; ++f) {
+            if (f + 1 < NF) read_v(va[(f + 1) & 1], f + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            const uint2 (&v)[2] = va[f & 1];
+            const u32x4_t vf = {v[0].x, v[0].y, v[1].x, v[1].y};
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) o[rt][f] = mfma16<DT>(vf, pf[rt], o[rt][f]);
+          }
+        } else {
+          // 0 x infinity is no number: with such a value among the keys, every row adds up the keys that it sees, one by one
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) l[rt] = mfma16<DT>(ones, pf[rt], l[rt]);
+#pragma unroll 1
+          for (int kk = 0; kk < 32; ++kk) {
+            const int x0 = 4 * (kk >> 4) + (kk & 3);         // which of the lane's probabilities
+            float pk[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+              uint32_t w = 0;
+#pragma unroll
+              for (int x = 0; x < 4; ++x) w |= (x0 >> 1) == x ? pf[rt][x] : 0u;
+              pk[rt] = __shfl(x0 & 1 ? hi_f32<DT>(w) : lo_f32<DT>(w), ((kk >> 2) & 3) * 16 + col, 64);
+            }
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+              int qq = quarter;
+              asm volatile("" : "+v"(qq));       // (an address of its own each time, not 2 NF running ones)
+              const uint2 v = *reinterpret_cast<const uint2 *>(vb + (32 * c + kk) * ROWB + (((2 * f + (qq >> 1)) ^ (kk & SW)) * 16) + (qq & 1) * 8);
+              const float x[4] = {lo_f32<DT>(v.x), hi_f32<DT>(v.x), lo_f32<DT>(v.y), hi_f32<DT>(v.y)};
+#pragma unroll
+              for (int rt = 0; rt < RT; ++rt)
+                if ((sees[rt] >> kk) & 1u) {
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) o[rt][f][i] += pk[rt] * x[i];
+                }
+            }
+          }
+        }
+      }
+    }
+
+    // ---- out: to the rows, where this workgroup had all their keys, else to the workspace
+    const bool whole = u0 == 0 && u1 == run.per_tile;
+    const long long which = 2LL * share + (u0 == 0 ? 1 : 0);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int r = (wave * RT + rt) * 16 + col;
+      if (r >= n_rows) continue;
+      const float ll = l[rt][0];
+      if (whole) {
+        const int gr = tile * ROWS + r, hh = gr - token[rt] * P.group;
+        uint16_t *op = P.out + (long long)(seq.row0 + token[rt]) * P.ldo + (long long)(h * P.group + hh) * D + 4 * quarter;
+        const float inv = ll > 0.0f || ll != ll ? 1.0f / ll : 0.0f;               // (no key seen: zeros)
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+          if (FULL || 16 * f + 4 * quarter < D)
+            *reinterpret_cast<uint2 *>(op + 16 * f) = make_uint2(pack2<DT>(o[rt][f][0] * inv, o[rt][f][1] * inv), pack2<DT>(o[rt][f][2] * inv, o[rt][f][3] * inv));
+      } else {
+        float *pp = P.part + (which * ROWS + r) * DP + 4 * quarter;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) *reinterpret_cast<f32x4_t *>(pp + 16 * f) = o[rt][f];
+        if (quarter == 0) P.part_ml[which * ROWS + r] = make_float2(m[rt], ll);
+      }
+    }
+    if (!whole && u0 == 0 && tid == 0) P.joins[share] = make_int4(s, h, tile, run.sharers());
+  } while (run.next(P));
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (rows loaded ahead and not used: their place in LDS is this workgroup's until they land)
 }
 
 // Joins the partial results of the tiles of rows whose keys several workgroups had: workgroup b takes the tile
