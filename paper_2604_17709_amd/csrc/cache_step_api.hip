@@ -65,7 +65,7 @@ int launch_attention_tiles(const AttPlan &pl, const AttParams &P, hipStream_t s)
     return fail(DEINFER_ERR_DEVICE, "tree attention: LDS size refused");
   hipLaunchKernelGGL((tree_attention_tile_kernel<DT, DP, FULL, POW2, RT>), dim3((unsigned)pl.shares), dim3(C::THREADS), C::LDS, s, P);
   if (int rc = check_launch("tree attention")) return rc;
-  hipLaunchKernelGGL((tree_attention_join_kernel<DT, DP, 128 * RT>), dim3((unsigned)pl.shares), dim3(JOIN_THREADS), 0, s, P);
+  hipLaunchKernelGGL((tree_attention_join_kernel<DT, DP, 128 * RT>), dim3((unsigned)pl.shares, 8 * RT), dim3(JOIN_THREADS<128 * RT>), 0, s, P);
   return check_launch("tree attention");
 }
 template <int DT, int DP, bool FULL, bool POW2>
@@ -75,7 +75,7 @@ int launch_attention(const AttPlan &pl, const AttParams &P, hipStream_t s) {
     if (pl.rows == 256) return launch_attention_tiles<DT, DP, FULL, POW2, 2>(pl, P, s);
   hipLaunchKernelGGL((tree_attention_kernel<DT, DP, FULL, POW2, 1, 4, 1>), dim3((unsigned)pl.shares), dim3(ATT_THREADS), 0, s, P);
   if (int rc = check_launch("tree attention")) return rc;
-  hipLaunchKernelGGL((tree_attention_join_kernel<DT, DP, 16>), dim3((unsigned)pl.shares), dim3(JOIN_THREADS), 0, s, P);
+  hipLaunchKernelGGL((tree_attention_join_kernel<DT, DP, 16>), dim3((unsigned)pl.shares), dim3(JOIN_THREADS<16>), 0, s, P);
   return check_launch("tree attention");
 }
 template <int DT, int DP>
