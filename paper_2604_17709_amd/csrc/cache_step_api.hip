@@ -160,7 +160,7 @@ int deinfer_tree_mask(const int32_t *parents, const int32_t *row_start, const in
   if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(&tree_mask_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                              tree_mask_lds(TREE_MAX_WORDS)) != hipSuccess)
     return fail(DEINFER_ERR_DEVICE, "tree mask: LDS size refused");
-  hipLaunchKernelGGL(tree_mask_kernel, dim3((unsigned)(n_seqs < 1024 ? n_seqs : 1024)), dim3(TREE_THREADS), (size_t)lds, static_cast<hipStream_t>(stream),
+  hipLaunchKernelGGL(tree_mask_kernel, dim3((unsigned)(n_seqs < 1024 ? n_seqs : 1024)), dim3(mask_words == 1 ? 256 : TREE_THREADS), (size_t)lds, static_cast<hipStream_t>(stream),
                      parents, row_start, cached, (int)n_seqs, (int)T, mask, (int)mask_words, positions);
   return check_launch("tree mask");
 }

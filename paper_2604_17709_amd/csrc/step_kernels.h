@@ -148,8 +148,9 @@ __global__ __launch_bounds__(STEP_THREADS) void kv_step_kernel(const KvStepParam
 }
 
 // ---- the plan of the compacting copy --------------------------------------------------------------
-constexpr int PLAN_IDS = 8;                                   // consecutive blocks of the walk per thread
+constexpr int PLAN_IDS = 2;                                   // consecutive blocks of the walk per thread
 constexpr int PLAN_CHUNK = STEP_THREADS * PLAN_IDS;           // blocks of the walk per workgroup
+constexpr int PLAN_AHEAD = 8;                                 // blocks per thread that are looked up together where they are only counted
 enum { KV_PLAN_BAD_BLOCK = 1, KV_PLAN_BUFFER_FULL = 2, KV_PLAN_TABLE_FULL = 4, KV_PLAN_RUNS_FULL = 8 };
 
 struct KvPlanParams {
@@ -162,8 +163,8 @@ struct KvPlanParams {
 // The walk goes through the sequences in table order and their blocks in logical order; block d of the
 // walk goes to block d of the buffer.  A block begins a run unless its physical id follows on that of
 // the block before it.  Workgroups 0 .. n_chunks - 1 write the runs of PLAN_CHUNK blocks each; the number
-// of runs before its chunk a workgroup counts by itself (one pass over the ids of the earlier chunks,
-// about a microsecond for every 8192 blocks, which is less than a second launch up to some 30000 blocks).
+// of runs before its chunk a workgroup counts by itself, in one pass over the ids of the earlier blocks: PLAN_AHEAD
+// look-ups of a thread go on side by side (a bisection in LDS, two loads), and there is one sum at the end.
 // The other workgroups write the remapped table and the positions.
 __global__ __launch_bounds__(STEP_THREADS) void kv_plan_kernel(const KvPlanParams P) {
   __shared__ int start[STEP_MAX_SEQS + 1];                    // first block of the walk of every sequence
@@ -196,8 +197,50 @@ __global__ __launch_bounds__(STEP_THREADS) void kv_plan_kernel(const KvPlanParam
     const int chunk = blockIdx.x, last_chunk = nb > 0 ? (nb - 1) / PLAN_CHUNK : 0;
     if (chunk > last_chunk) return;
     int runs = 0, last_head = 0;                              // of the chunks before
-    for (int c = 0; c <= chunk; ++c) {
-      const int d0 = c * PLAN_CHUNK + tid * PLAN_IDS;
+    if (chunk > 0) {
+      const int before = chunk * PLAN_CHUNK;                  // (all below nb)
+      int count = 0, top = 0;
+      // a wavefront's 64 PLAN_AHEAD blocks in a row: one bisection, from there on each lane steps along
+      for (int d0 = (tid >> 6) * 64 * PLAN_AHEAD; d0 < before; d0 += STEP_THREADS * PLAN_AHEAD) {
+        const int lane = tid & 63, d_prev = d0 > 0 ? d0 - 1 : 0;
+        int s = last_not_above(start, n, d_prev), from = start[s], next = start[s + 1];
+        const int *row = P.table + s * P.table_pitch - from;
+        int prev = d0 > 0 ? row[d_prev] : -1, id[PLAN_AHEAD];
+#pragma unroll
+        for (int i = 0; i < PLAN_AHEAD; ++i) {
+          const int d = d0 + 64 * i + lane;
+          id[i] = -1;
+          if (d >= before) continue;
+          while (next <= d) {
+            row += P.table_pitch - (next - from);             // (a row is addressed by the walk's numbers)
+            from = next;
+            next = start[++s + 1];
+          }
+          id[i] = row[d];
+        }
+#pragma unroll
+        for (int i = 0; i < PLAN_AHEAD; ++i) {
+          const int d = d0 + 64 * i + lane;
+          int p = __shfl_up(id[i], 1, 64);
+          if (lane == 0) p = prev;
+          prev = __shfl(id[i], 63, 64);
+          if (d >= before) continue;
+          const bool good = id[i] >= 0 && id[i] < P.n_pool_blocks;
+          if (!good) flags |= KV_PLAN_BAD_BLOCK;
+          if (!good || p < 0 || (uint32_t)id[i] != (uint32_t)p + 1u) { ++count; top = d; }      // (p outside the pool has no follower inside)
+        }
+      }
+      block_scan(count, scratch, &runs);
+      const int lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) { const int u = __shfl_xor(top, o, 64); top = u > top ? u : top; }
+      __syncthreads();
+      if (lane == 0) scratch[wave] = top;
+      __syncthreads();
+      for (int w = 0; w < STEP_THREADS / 64; ++w) last_head = scratch[w] > last_head ? scratch[w] : last_head;
+    }
+    {
+      const int d0 = chunk * PLAN_CHUNK + tid * PLAN_IDS;
       // ids of the blocks d0 - 1 .. d0 + PLAN_IDS of the walk; -1: none, or outside the pool
       int id[PLAN_IDS + 2];
       const int from = d0 > 0 ? d0 - 1 : 0;
@@ -243,7 +286,7 @@ __global__ __launch_bounds__(STEP_THREADS) void kv_plan_kernel(const KvPlanParam
       }
       int open = __shfl_up(carry, 1, 64);                      // head of the run that is open before my first block
       if (lane == 0 || open < wave_before) open = wave_before;
-      if (c == chunk) {
+      {
         int r = runs + end - mine - 1;                         // index of the run that is open
 #pragma unroll
         for (int i = 0; i < PLAN_IDS; ++i) {
@@ -295,7 +338,7 @@ __global__ __launch_bounds__(STEP_THREADS) void kv_plan_kernel(const KvPlanParam
 }
 
 // ---- drafted trees ------------------------------------------------------------------------------
-constexpr int TREE_THREADS = 256;
+constexpr int TREE_THREADS = 1024;                           // 256 for drafts of one word
 constexpr int TREE_MAX_WORDS = 32;
 
 // LDS of tree_mask_kernel in bytes: the bits of 32 words rows (one word of padding per row), two lists of ancestors
@@ -312,6 +355,8 @@ __global__ __launch_bounds__(TREE_THREADS) void tree_mask_kernel(const int *pare
   uint32_t *bits = reinterpret_cast<uint32_t *>(tree_smem);    // [32 words][words + 1]
   const int most = 32 * words, pitch = words + 1;
   int *anc = reinterpret_cast<int *>(bits + most * pitch);     // [2][32 words]
+  const int threads = blockDim.x, tid = threadIdx.x, rows_at_once = threads / words;
+  const int w = tid % words, j_first = tid < rows_at_once * words ? tid / words : INT32_MAX / 2;      // this thread's word of rows j_first + rows_at_once i
   for (int s = blockIdx.x; s < n_seqs; s += gridDim.x) {
     int r0 = row_start[s], r1 = row_start[s + 1];
     r0 = r0 < 0 ? 0 : r0; r1 = r1 > T ? T : r1;
@@ -319,23 +364,20 @@ __global__ __launch_bounds__(TREE_THREADS) void tree_mask_kernel(const int *pare
     const int rows = r1 - r0, n = rows < most ? rows : most;
     int c = cached[s];
     c = c < 0 ? 0 : c;
-    for (int j = threadIdx.x; j < n; j += TREE_THREADS) {
+    for (int j = tid; j < n; j += threads) {
       const int p = parents[r0 + j];
       anc[j] = p >= 0 && p < j ? p : -1;
     }
-    for (int x = threadIdx.x; x < n * words; x += TREE_THREADS) {
-      const int j = x / words, w = x - j * words;
-      bits[j * pitch + w] = j / 32 == w ? 1u << (j & 31) : 0u;
-    }
+    for (int j = j_first; j < n; j += rows_at_once) bits[j * pitch + w] = j / 32 == w ? 1u << (j & 31) : 0u;
     __syncthreads();
     int *from = anc, *to = anc + most;
     for (int span = 1; span < n; span *= 2) {                  // (an ancestor is at most n - 1 steps away)
       int more = 0;
-      for (int x = threadIdx.x; x < n * words; x += TREE_THREADS) {
-        const int j = x / words, w = x - j * words, a = from[j];
+      for (int j = j_first; j < n; j += rows_at_once) {
+        const int a = from[j];
         if (a >= 0) bits[j * pitch + w] |= bits[a * pitch + w];
       }
-      for (int j = threadIdx.x; j < n; j += TREE_THREADS) {
+      for (int j = tid; j < n; j += threads) {
         const int a = from[j], b = a >= 0 ? from[a] : -1;
         to[j] = b;
         more |= b >= 0;
@@ -344,15 +386,12 @@ __global__ __launch_bounds__(TREE_THREADS) void tree_mask_kernel(const int *pare
       int *t = from; from = to; to = t;
     }
     __syncthreads();
-    for (long long x = threadIdx.x; x < (long long)rows * words; x += TREE_THREADS) {
-      const int j = (int)(x / words), w = (int)(x - (long long)j * words);
-      mask[(long long)(r0 + j) * words + w] = j < n ? bits[j * pitch + w] : 0u;
-    }
+    for (int j = j_first; j < rows; j += rows_at_once) mask[(long long)(r0 + j) * words + w] = j < n ? bits[j * pitch + w] : 0u;
     if (positions)
-      for (int j = threadIdx.x; j < rows; j += TREE_THREADS) {
+      for (int j = tid; j < rows; j += threads) {
         int depth = 0;
         if (j < n) {
-          for (int w = 0; w < words; ++w) depth += __popc(bits[j * pitch + w]);
+          for (int i = 0; i < words; ++i) depth += __popc(bits[j * pitch + i]);
           --depth;
         }
         const long long p = (long long)c + depth;
