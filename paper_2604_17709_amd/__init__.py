@@ -527,7 +527,10 @@ def deinfer_lowrank_gateup_silu(x, fgate: Pair, fup: Pair, ws: Workspace, out=No
 def _on_device(*tensors) -> None:
     """The library takes pointers of the current device: anything else is refused here, before a kernel reads it."""
     import torch
-    here = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+    try:
+        here = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
+    except AttributeError:
+        here = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"tensors of the current device (cuda:{here}) expected, got one on {t.device}")
@@ -539,6 +542,17 @@ def _ints(what: str, t, n: Optional[int] = None):
     if t.dtype != torch.int32 or not t.is_contiguous() or (n is not None and t.numel() < n):
         raise ValueError(f"{what}: contiguous int32 tensor{'' if n is None else f' of at least {n} values'} expected")
     return t
+
+
+def _matrix(x, what: str):
+    """Rows, columns and pitch of a row-major 2-D tensor: ``_rows`` and ``_ld`` in one look at it."""
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError(f"{what} must be a row-major 2-D tensor")
+    (rows, cols), (pitch, step) = shape, x.stride()
+    if cols and step != 1:
+        raise ValueError(f"{what} must be a row-major 2-D tensor")
+    return rows, cols, max(pitch if rows > 1 or pitch >= cols else cols, 1)
 
 
 def _table(t, n_seqs: int) -> int:
@@ -578,10 +592,16 @@ def deinfer_kv_step(cached, n_new, block_table, free_list, block_tokens: int, n_
     if free_first is not None:
         _ints("free_first", free_first, 1)
     if out is None:
-        out = KvStep(*(_new(k, torch.int32, cached.device, stream) for k in (n + 1, int(rows), int(rows), 4)))
-    for name, t, k in zip(KvStep._fields, out, (n + 1, rows, rows, 4)):
-        _ints(name, t, k)
-    _on_device(cached, n_new, block_table, free_list, free_first, *out)
+        # one allocation: row_start and counts ahead of slots and positions, which begin at whole 16 bytes
+        head, each = (n + 8) & ~3, (int(rows) + 3) & ~3
+        start, _, counts, slots, _, positions = _new(head + each + int(rows), torch.int32, cached.device, stream).split_with_sizes(
+            (n + 1, head - n - 5, 4, int(rows), each - int(rows), int(rows)))
+        out = KvStep(start, slots, positions, counts)
+        _on_device(cached, n_new, block_table, free_list, free_first)
+    else:
+        for name, t, k in zip(KvStep._fields, out, (n + 1, rows, rows, 4)):
+            _ints(name, t, k)
+        _on_device(cached, n_new, block_table, free_list, free_first, *out)
     _check(lib().deinfer_kv_step(_ptr(cached), _ptr(n_new), n, _ptr(free_list), free_list.numel(), _ptr(free_first), int(n_pool_blocks),
                                  int(block_tokens), _ptr(block_table), pitch, int(rows), _ptr(out.row_start), _ptr(out.slots),
                                  _ptr(out.positions), _ptr(out.counts), _stream(stream)))
@@ -600,15 +620,17 @@ def deinfer_kv_compact_plan_device(block_table, n_tokens, n_pool_blocks: int, bu
     if out is None:
         cap = int(buffer_blocks if capacity_runs is None else capacity_runs)
         dev = n_tokens.device
-        out = (_new(KV_PLAN_HEADER + 3 * cap, torch.int32, dev, stream), _new((n, pitch), torch.int32, dev, stream),
-               _new(int(buffer_blocks) * int(block_tokens), torch.int32, dev, stream))
-    plan, remap, positions = out
-    _ints("plan", plan, KV_PLAN_HEADER)
-    if remap is not None:
-        _table(remap, n)
-    if positions is not None:
-        _ints("positions", positions, int(buffer_blocks) * int(block_tokens))
-    _on_device(block_table, n_tokens, n_new, plan, remap, positions)
+        plan, remap, positions = (_new(KV_PLAN_HEADER + 3 * cap, torch.int32, dev, stream), _new((n, pitch), torch.int32, dev, stream),
+                                  _new(int(buffer_blocks) * int(block_tokens), torch.int32, dev, stream))
+        _on_device(block_table, n_tokens, n_new)
+    else:
+        plan, remap, positions = out
+        _ints("plan", plan, KV_PLAN_HEADER)
+        if remap is not None:
+            _table(remap, n)
+        if positions is not None:
+            _ints("positions", positions, int(buffer_blocks) * int(block_tokens))
+        _on_device(block_table, n_tokens, n_new, plan, remap, positions)
     _check(lib().deinfer_kv_compact_plan_device(_ptr(block_table), n, pitch, _ptr(n_tokens), _ptr(n_new), int(n_pool_blocks),
                                                 int(buffer_blocks), int(block_tokens), _ptr(plan), (plan.numel() - KV_PLAN_HEADER) // 3,
                                                 _ptr(remap), 0 if remap is None else remap.shape[1], _ptr(positions), _stream(stream)))
@@ -652,38 +674,47 @@ def deinfer_rope_store(q, k, v, positions, freqs, n_q_heads: int, n_kv_heads: in
     """Queries rotated, keys rotated and values copied into their slots of the cache.  q, k and v may each be None; q_out, k_out
     and v_out default to them (k and v: without slots only).  freqs: float64 device tensor [rot_dim / 2], or None to copy."""
     import torch
-    given = [t for t in (q, k, v) if t is not None]
-    if not given:
+    first = q if q is not None else k if k is not None else v
+    if first is None:
         return q_out, k_out, v_out
-    rows = _rows(given[0], "rows")
+    rows, dtype = (first.shape[0] if first.dim() else 0), first.dtype
     q_out = q if q_out is None else q_out
     if slots is None:
         k_out, v_out = (k if k_out is None else k_out), (v if v_out is None else v_out)
     elif (k is not None and k_out is None) or (v is not None and v_out is None):
         raise ValueError("with slots, k_out and v_out (the pools) are needed")
-    n_slots = None
+    n_slots, args = None, []                     # args: pointer and pitch of each tensor and of where it goes
     for what, t, to, heads in (("q", q, q_out, n_q_heads), ("k", k, k_out, n_kv_heads), ("v", v, v_out, n_kv_heads)):
         if t is None:
+            args.append((None, 0, None, 0))
             continue
         pooled = slots is not None and what != "q"
-        if _rows(t, what) != rows or t.shape[1] < heads * head_dim or to.dtype != t.dtype or t.dtype != given[0].dtype:
+        have, cols, ld = _matrix(t, what)
+        if have != rows or cols < heads * head_dim or t.dtype != dtype:
             raise ValueError(f"{what}: [rows, heads * head_dim] of one dtype expected")
-        if _rows(to, what + "_out") < (0 if pooled else rows) or to.shape[1] < heads * head_dim:
-            raise ValueError(f"{what}_out: too small")
+        if to is t:
+            args.append((t.data_ptr(), ld, t.data_ptr(), ld))
+        else:
+            room, cols, ldo = _matrix(to, what + "_out")
+            if to.dtype != dtype:
+                raise ValueError(f"{what}: [rows, heads * head_dim] of one dtype expected")
+            if room < (0 if pooled else rows) or cols < heads * head_dim:
+                raise ValueError(f"{what}_out: too small")
+            args.append((t.data_ptr(), ld, to.data_ptr(), ldo))
         if pooled:
             n_slots = to.shape[0] if n_slots is None else min(n_slots, to.shape[0])
-    if freqs is not None and (freqs.dtype != torch.float64 or not freqs.is_contiguous()):
-        raise ValueError("freqs: contiguous float64 tensor expected")
-    if freqs is not None and freqs.numel():
-        _ints("positions", positions, rows)
+    if freqs is not None:
+        if freqs.dtype != torch.float64 or not freqs.is_contiguous():
+            raise ValueError("freqs: contiguous float64 tensor expected")
+        if freqs.numel():
+            _ints("positions", positions, rows)
     if slots is not None:
         _ints("slots", slots, rows)
-    _on_device(q, k, v, positions, freqs, slots, q_out if q is not None else None, k_out if k is not None else None, v_out if v is not None else None)
-    p = lambda t, to: (None, 0, None, 0) if t is None else (_ptr(t), _ld(t), _ptr(to), _ld(to))
-    (qp, ldq, qo, ldqo), (kp, ldk, ko, ldko), (vp, ldv, vo, ldvo) = p(q, q_out), p(k, k_out), p(v, v_out)
+    _on_device(q, k, v, positions, freqs, slots, None if q_out is q or q is None else q_out, None if k_out is k or k is None else k_out, None if v_out is v or v is None else v_out)
+    (qp, ldq, qo, ldqo), (kp, ldk, ko, ldko), (vp, ldv, vo, ldvo) = args
     _check(lib().deinfer_rope_store(qp, ldq, int(n_q_heads), kp, ldk, vp, ldv, int(n_kv_heads), rows, int(head_dim),
                                     0 if freqs is None else 2 * freqs.numel(), int(interleaved), _ptr(positions), _ptr(freqs), float(magnitude),
-                                    _ptr(slots), n_slots or 0, qo, ldqo, ko, ldko, vo, ldvo, _dtype_code(given[0]), _stream(stream)))
+                                    _ptr(slots), n_slots or 0, qo, ldqo, ko, ldko, vo, ldvo, _dtype_code(first), _stream(stream)))
     return q_out, k_out, v_out
 
 
@@ -697,14 +728,14 @@ def deinfer_tree_attention(q, k_pool, v_pool, block_table, row_start, cached, ws
                            scale: Optional[float] = None, mask=None, out=None, stream=None):
     """Attention of a step's rows over the paged cache: k_pool, v_pool [slots, n_kv_heads * head_dim]; mask: int32 [rows, words]
     visibility bits among a sequence's own rows (None: causal).  Rows behind the last sequence's keep what ``out`` holds."""
-    rows, n = _rows(q, "q"), cached.numel()
-    if n_q_heads <= 0 or q.shape[1] % n_q_heads:
+    (rows, cols, ldq), n = _matrix(q, "q"), cached.numel()
+    if n_q_heads <= 0 or cols % n_q_heads:
         raise ValueError("q: [rows, n_q_heads * head_dim] expected")
-    head_dim = q.shape[1] // n_q_heads
-    n_slots = _rows(k_pool, "k_pool")
-    if _rows(v_pool, "v_pool") != n_slots or k_pool.shape[1] < n_kv_heads * head_dim or v_pool.shape[1] < n_kv_heads * head_dim:
+    head_dim, dtype = cols // n_q_heads, q.dtype
+    (n_slots, k_cols, ldk), (v_slots, v_cols, ldv) = _matrix(k_pool, "k_pool"), _matrix(v_pool, "v_pool")
+    if v_slots != n_slots or k_cols < n_kv_heads * head_dim or v_cols < n_kv_heads * head_dim:
         raise ValueError("k_pool, v_pool: [slots, n_kv_heads * head_dim] expected")
-    if k_pool.dtype != q.dtype or v_pool.dtype != q.dtype:
+    if k_pool.dtype != dtype or v_pool.dtype != dtype:
         raise ValueError("q, k_pool and v_pool must share a dtype")
     _ints("cached", cached)
     _ints("row_start", row_start, n + 1)
@@ -716,12 +747,14 @@ def deinfer_tree_attention(q, k_pool, v_pool, block_table, row_start, cached, ws
             raise ValueError("mask: [rows, words] expected")
         words = mask.shape[1]
     if out is None:
-        out = _new((rows, n_q_heads * head_dim), q.dtype, q.device, stream)
-    elif out.dtype != q.dtype or _rows(out, "out") < rows or out.shape[1] < n_q_heads * head_dim:
-        raise ValueError("out: [rows, n_q_heads * head_dim] of q's dtype expected")
+        out, ldo = _new((rows, cols), dtype, q.device, stream), max(cols, 1)
+    else:
+        out_rows, out_cols, ldo = _matrix(out, "out")
+        if out.dtype != dtype or out_rows < rows or out_cols < cols:
+            raise ValueError("out: [rows, n_q_heads * head_dim] of q's dtype expected")
     _on_device(q, k_pool, v_pool, block_table, row_start, cached, mask, out, ws.buf)
-    _check(lib().deinfer_tree_attention(_ptr(q), rows, _ld(q), int(n_q_heads), int(n_kv_heads), head_dim, _ptr(row_start), _ptr(cached), n,
-                                        _ptr(mask), words, _ptr(k_pool), _ld(k_pool), _ptr(v_pool), _ld(v_pool), n_slots // int(block_tokens),
+    _check(lib().deinfer_tree_attention(_ptr(q), rows, ldq, int(n_q_heads), int(n_kv_heads), head_dim, _ptr(row_start), _ptr(cached), n,
+                                        _ptr(mask), words, _ptr(k_pool), ldk, _ptr(v_pool), ldv, n_slots // int(block_tokens),
                                         int(block_tokens), _ptr(block_table), pitch, head_dim ** -0.5 if scale is None else float(scale),
-                                        _ptr(out), _ld(out), _dtype_code(q), _ptr(ws.buf), ws.nbytes, _stream(stream)))
+                                        _ptr(out), ldo, _dtype_code(q), _ptr(ws.buf), ws.nbytes, _stream(stream)))
     return out
