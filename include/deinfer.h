@@ -431,11 +431,14 @@ int deinfer_rope_store(const void *q, int64_t ldq, int64_t n_q_heads,
  * influence, infinities and NaN included.  Padding rows of out are left as they are.
  *   q, out: T x (n_q_heads head_dim), pitches ldq, ldo; k_pool, v_pool: n_pool_blocks * block_tokens rows of n_kv_heads
  *   head_dim, pitches ldk, ldv; block_table: device int32 [n_seqs][table_pitch], at least ceil((cached + rows) /
- *   block_tokens) entries of a row in use.  dtype: bf16 or fp16.  head_dim: a multiple of 8, at most 256.  scale > 0.
+ *   block_tokens) entries of a row in use.  dtype: bf16 or fp16.  head_dim: a multiple of 8, at most 256.  scale: a normal
+ *   positive number of fp32, with 1 / ln 2 on it too.
  *   q, pools and out 16-byte aligned, pitches multiples of 8.  out must not overlap q.
  * Scores, maxima, sums and outputs are fp32; the probabilities are rounded to the storage type for the second product, the
  * output is rounded once.  Results do not depend on timing.  The workspace (deinfer_tree_attention_workspace_bytes,
- * host only; 256-byte aligned) needs no clearing and serves one call at a time.  T <= 2^28, T n_q_heads < 2^30.
+ * host only; 256-byte aligned) needs no clearing and serves one call at a time.  Its size is that of the call's own T
+ * and n_seqs: more rows need no less, fewer sequences with the same rows may need more.  T <= 2^28, T n_q_heads < 2^30,
+ * table_pitch block_tokens <= 2^30.
  */
 int deinfer_tree_attention_workspace_bytes(int64_t T, int64_t n_seqs, int64_t n_q_heads, int64_t n_kv_heads,
                                            int64_t head_dim, size_t *bytes);

@@ -279,6 +279,8 @@ int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_he
   if (dtype != DEINFER_BF16 && dtype != DEINFER_F16) return fail(DEINFER_ERR_UNSUPPORTED, "tree attention: 16-bit types (bf16, fp16) only");
   if (head_dim <= 0 || head_dim % 8 != 0 || head_dim > 256) return fail(DEINFER_ERR_UNSUPPORTED, "tree attention: head_dim must be a multiple of 8, from 8 to 256");
   if (!(scale > 0.0) || !std::isfinite(scale)) return fail(DEINFER_ERR_INVALID_ARG, "tree attention: scale must be positive");
+  const float scale2 = (float)(scale * 1.4426950408889634074);      // (0 or infinity times a score would be no number)
+  if (!std::isnormal(scale2)) return fail(DEINFER_ERR_UNSUPPORTED, "tree attention: scale is out of the range of fp32");
   if (T > MAX_ROWS || n_q_heads > MAX_PITCH / head_dim || T * n_q_heads > INT32_MAX / 2) return fail(DEINFER_ERR_UNSUPPORTED, "tree attention: sizes out of range");
   if (mask && (mask_words <= 0 || mask_words > DEINFER_TREE_MAX_WORDS)) return fail(DEINFER_ERR_INVALID_ARG, "tree attention: mask_words must be from 1 to %d", DEINFER_TREE_MAX_WORDS);
   const int64_t wq = n_q_heads * head_dim, wk = n_kv_heads * head_dim;
@@ -306,7 +308,7 @@ int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_he
   P.block_tokens = (int)block_tokens; P.mask_words = (int)mask_words;
   P.block_shift = 0;
   if ((block_tokens & (block_tokens - 1)) == 0) while ((1LL << P.block_shift) < block_tokens) ++P.block_shift;
-  P.scale2 = (float)(scale * 1.4426950408889634074);
+  P.scale2 = scale2;
   P.n_shares = (int)pl.shares;
   char *w = static_cast<char *>(ws);
   P.joins = reinterpret_cast<int4 *>(w + pl.joins);

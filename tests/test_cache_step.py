@@ -101,6 +101,18 @@ def test_attention_refusals():
     assert attend(T=0, q=None) == dn.OK and attend(n_seqs=0, q=None) == dn.OK
 
 
+def test_attention_refuses_a_scale_that_fp32_cannot_hold():
+    for scale in (1e-46, 1e-39, 3e38, 1e300):
+        assert attend(scale=scale) == dn.ERR_UNSUPPORTED, scale
+
+
+def test_a_call_with_fewer_sequences_may_need_a_larger_workspace():
+    """More rows per sequence take larger tiles; with as many sequences, more rows never need less."""
+    sizes = [dn.deinfer_tree_attention_workspace_bytes(T, 8, 32, 8, 128) for T in (1, 8, 33, 300, 600, 5000)]
+    assert sizes == sorted(sizes)
+    assert dn.deinfer_tree_attention_workspace_bytes(600, 2, 32, 8, 128) > dn.deinfer_tree_attention_workspace_bytes(600, 600, 32, 8, 128)
+
+
 def test_attention_workspace_refusals():
     for bad in ((-1, 1, 1, 1, 64), (1, -1, 1, 1, 64), (1, 1, 0, 1, 64), (1, 1, 4, 3, 64), (1, 1, 1, 1, 0)):
         with pytest.raises(dn.DeinferError) as e:
