@@ -539,7 +539,7 @@ def _on_device(*tensors) -> None:
 def _ints(what: str, t, n: Optional[int] = None):
     """A contiguous int32 list of at least n values."""
     import torch
-    if t.dtype != torch.int32 or not t.is_contiguous() or (n is not None and t.numel() < n):
+    if t is None or t.dtype != torch.int32 or not t.is_contiguous() or (n is not None and t.numel() < n):
         raise ValueError(f"{what}: contiguous int32 tensor{'' if n is None else f' of at least {n} values'} expected")
     return t
 

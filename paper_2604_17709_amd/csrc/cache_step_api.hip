@@ -77,7 +77,7 @@ int launch_attention(const AttPlan &pl, const AttParams &P, hipStream_t s) {
   if (pl.rows == 128) return launch_attention_tiles<DT, DP, FULL, POW2, 1>(pl, P, s);
   if constexpr (DP < 256)
     if (pl.rows == 256) return launch_attention_tiles<DT, DP, FULL, POW2, 2>(pl, P, s);
-  hipLaunchKernelGGL((tree_attention_kernel<DT, DP, FULL, POW2, 1, 4, 1>), dim3((unsigned)pl.shares), dim3(ATT_THREADS), 0, s, P);
+  hipLaunchKernelGGL((tree_attention_kernel<DT, DP, FULL, POW2>), dim3((unsigned)pl.shares), dim3(ATT_THREADS), 0, s, P);
   if (int rc = check_launch("tree attention")) return rc;
   hipLaunchKernelGGL((tree_attention_join_kernel<DT, DP, 16>), dim3((unsigned)pl.shares), dim3(JOIN_THREADS<16>), 0, s, P);
   return check_launch("tree attention");
@@ -91,7 +91,7 @@ int launch_attention_of(const AttPlan &pl, const AttParams &P, hipStream_t s) {
 
 template <typename TE>
 void launch_rope_store(const RopeStoreParams &P, bool vec, bool inter, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)P.T * P.parts)), block(ROPE_THREADS);
+  const dim3 grid((unsigned)P.T), block(ROPE_THREADS);
   if (vec && inter) hipLaunchKernelGGL((rope_store_kernel<TE, 16 / sizeof(TE), true>), grid, block, 0, s, P);
   else if (vec) hipLaunchKernelGGL((rope_store_kernel<TE, 16 / sizeof(TE), false>), grid, block, 0, s, P);
   else if (inter) hipLaunchKernelGGL((rope_store_kernel<TE, 2, true>), grid, block, 0, s, P);
@@ -254,8 +254,6 @@ int deinfer_rope_store(const void *q, int64_t ldq, int64_t n_q_heads, const void
   P.ldq = ldq; P.ldk = ldk; P.ldv = ldv; P.ldqo = ldqo; P.ldko = ldko; P.ldvo = ldvo; P.n_slots = n_slots;
   P.T = (int)T; P.n_q = have_q ? (int)n_q_heads : 0; P.n_kv = have_k ? (int)n_kv_heads : 0; P.n_v = have_v ? (int)n_kv_heads : 0;
   P.head_dim = (int)head_dim; P.rot_dim = have_q || have_k ? (int)rot_dim : 0; P.magnitude = (float)magnitude;
-  P.parts = 1;
-  if (T * P.parts > INT32_MAX) return fail(DEINFER_ERR_UNSUPPORTED, "rope store: too many tokens");
   by_dtype(dtype, [&](auto tag) {
     launch_rope_store<decltype(tag)>(P, vec, interleaved != 0, static_cast<hipStream_t>(stream));
     return 0;

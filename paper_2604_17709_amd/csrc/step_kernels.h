@@ -59,7 +59,7 @@ struct KvStepParams {
 // ceil(c / b) .. ceil((c + m) / b) - 1 are new; the new blocks of all sequences, counted in order, take
 // the free list's entries in order.  Entries of the table below ceil(c / b) are read, those from there
 // on are written, so no workgroup reads what another writes; a new block is written by the row of
-// its first token.
+// its first token.  8 us for 8 sequences (a call takes the host 11.5), 13.5 for 2048 sequences and 8000 rows.
 __global__ __launch_bounds__(STEP_THREADS) void kv_step_kernel(const KvStepParams P) {
   __shared__ int row_start[STEP_MAX_SEQS + 1];
   __shared__ int need_start[STEP_MAX_SEQS + 1];
@@ -165,7 +165,8 @@ struct KvPlanParams {
 // the block before it.  Workgroups 0 .. n_chunks - 1 write the runs of PLAN_CHUNK blocks each; the number
 // of runs before its chunk a workgroup counts by itself, in one pass over the ids of the earlier blocks: PLAN_AHEAD
 // look-ups of a thread go on side by side (a bisection in LDS, two loads), and there is one sum at the end.
-// The other workgroups write the remapped table and the positions.
+// The other workgroups write the remapped table and the positions.  7.7 us for 16 sequences of 32 blocks; 33 us for 1024 sequences
+// and 66000 blocks, of which 18 are the last workgroup's count and 4 the words behind the last run.
 __global__ __launch_bounds__(STEP_THREADS) void kv_plan_kernel(const KvPlanParams P) {
   __shared__ int start[STEP_MAX_SEQS + 1];                    // first block of the walk of every sequence
   __shared__ long long scratch64[STEP_THREADS / 64];
@@ -349,6 +350,7 @@ __host__ __device__ constexpr int tree_mask_lds(int words) { return 4 * (32 * wo
 // that row's pointer.  ceil(log2(depth)) rounds instead of a walk of `depth` dependent steps.  A row may
 // read bits that their owner has already extended in the same round: those are ancestors too, and the pointers
 // are kept in two lists, so every round does what it has to.  The depth is the number of bits less one.
+// 4.2 us for 16 drafts of 8 tokens, 8.7 for 256 of 256 (256 threads and a division per word: 17).
 __global__ __launch_bounds__(TREE_THREADS) void tree_mask_kernel(const int *parents, const int *row_start, const int *cached, int n_seqs, int T,
                                                                  uint32_t *mask, int words, int *positions) {
   extern __shared__ __attribute__((aligned(16))) unsigned char tree_smem[];

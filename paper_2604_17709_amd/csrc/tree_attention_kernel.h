@@ -207,23 +207,24 @@ template <int DT> __device__ __forceinline__ bool not_finite(uint32_t w) {
 
 // DP: head dimension up to 64, 128 or 256; FULL: it is DP; POW2: blocks of a power of two of at least 16
 // tokens (16 neighbouring keys are rows of one block: their address is one scalar and a lane's constant);
-// WR x WK wavefronts, WR row groups of RT tiles of 16 rows, each over WK interleaved shares of the keys.
-template <int DT, int DP, bool FULL, bool POW2, int WR, int WK, int RT>
+// one tile of 16 rows, over four wavefronts' interleaved shares of the keys, which are merged in LDS.
+// Bound by reading the cache: 64 sequences of up to 8191 cached tokens, 8 key heads of 128, one token each: 217 us for 1.13 GB =
+// 5.2 TB/s (a read alone: 6.0); three workgroups per unit in fewer registers: 225, four: 266.  8 sequences of up to 1000: 11.5 us,
+// which is one dependent chain: lengths, block ids, rows, merge.
+template <int DT, int DP, bool FULL, bool POW2>
 __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttParams P) {
-  static_assert(WR * WK * 64 == ATT_THREADS, "four wavefronts");
-  constexpr int ROWS = 16 * WR * RT, UNIT = ATT_KEYS * WK;
+  constexpr int WK = ATT_THREADS / 64, ROWS = 16, UNIT = ATT_KEYS * WK;
   constexpr int KS = DP / 32;                    // k steps of the first product
   constexpr int VE = DP == 64 ? 4 : 8;           // neighbouring features of V per lane and piece
   constexpr int NC = DP / (16 * VE);             // pieces
   constexpr int NF = NC * VE;                    // 16-feature blocks of the output
   constexpr int VW = VE / 2;                     // words of a piece
   constexpr int OP = DP + 4;                     // row pitch of the merge buffer in LDS
-  __shared__ __attribute__((aligned(16))) float merge_o[WK > 1 ? WK * 16 * OP : 4];
-  __shared__ float merge_ml[WK > 1 ? 2 * WK * 16 : 2];
+  __shared__ __attribute__((aligned(16))) float merge_o[WK * 16 * OP];
+  __shared__ float merge_ml[2 * WK * 16];
   __shared__ long long scan[ATT_THREADS / 64];
   __shared__ long long found[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wr = wave / WK, wk = wave % WK;
   const int col = lane & 15, quarter = lane >> 4;
   const int D = FULL ? DP : P.head_dim;
   const int share = run_tile_of(blockIdx.x, P.n_shares);
@@ -237,28 +238,20 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
 
     // ---- the rows
     const int n_rows = seq.n * P.group - tile * ROWS < ROWS ? seq.n * P.group - tile * ROWS : ROWS;   // of this tile
-    u32x4_t qf[RT][KS];
-    int token[RT];                               // of this lane's row of every row tile
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int r = (wr * RT + rt) * 16 + col, gr = tile * ROWS + r;
-      const int j = gr / P.group, hh = gr - j * P.group;
-      token[rt] = j;
-      const uint16_t *qp = P.q + (long long)(seq.row0 + j) * P.ldq + (long long)(h * P.group + hh) * D + quarter * 8;
+    const int gr = tile * ROWS + col, token = gr / P.group;           // this lane's row
+    u32x4_t qf[KS];
+    {
+      const uint16_t *qp = P.q + (long long)(seq.row0 + token) * P.ldq + (long long)(h * P.group + gr - token * P.group) * D + quarter * 8;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        qf[rt][ks] = u32x4_t{0u, 0u, 0u, 0u};
-        if (r < n_rows && (FULL || ks * 32 + quarter * 8 < D)) qf[rt][ks] = *reinterpret_cast<const u32x4_t *>(qp + ks * 32);
+        qf[ks] = u32x4_t{0u, 0u, 0u, 0u};
+        if (col < n_rows && (FULL || ks * 32 + quarter * 8 < D)) qf[ks] = *reinterpret_cast<const u32x4_t *>(qp + ks * 32);
       }
     }
-    f32x4_t o[RT][NF];
-    float m[RT], l[RT];
+    f32x4_t o[NF];
+    float m = -__builtin_inff(), l = 0.0f;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      m[rt] = -__builtin_inff(); l[rt] = 0.0f;
-#pragma unroll
-      for (int f = 0; f < NF; ++f) o[rt][f] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    }
+    for (int f = 0; f < NF; ++f) o[f] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     // keys that some row may see, and keys that every row sees
     const int keys_end = att_tile_keys<ROWS>(P, seq, tile);
     const int keys_all = P.mask ? seq.ctx : seq.ctx + tile * ROWS / P.group + 1;
@@ -267,7 +260,7 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
     const char *kh = reinterpret_cast<const char *>(P.k + (long long)h * D), *vh = reinterpret_cast<const char *>(P.v + (long long)h * D);
     const uint32_t klane = col * P.ldk + quarter * 16, vlane = quarter * 4 * P.ldv + col * VE * 2;
     const int k_last = u1 * UNIT < keys_end ? u1 * UNIT : keys_end;
-    for (int k0 = u0 * UNIT + wk * ATT_KEYS; k0 < k_last; k0 += UNIT) {
+    for (int k0 = u0 * UNIT + wave * ATT_KEYS; k0 < k_last; k0 += UNIT) {
       // ---- where the 32 keys are; `live`: those that exist
       uint32_t live = keys_end - k0 >= 32 ? 0xffffffffu : (1u << (keys_end - k0)) - 1u;
       const char *kp[2], *vp[2];                 // POW2: rows of the two halves' first keys
@@ -330,7 +323,7 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
       }
       // ---- what each row sees of the 32 keys
       const bool masked = live != 0xffffffffu || k0 + 32 > keys_all;
-      uint32_t sees[RT];
+      uint32_t sees = 0xffffffffu;
       bool odd_v = false;                        // a value that is infinite or NaN beside rows that do not see it
       if (masked) {
 #pragma unroll
@@ -345,85 +338,78 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
             }
         }
         odd_v = __any(odd_v);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          const uint32_t w = att_window(P, seq, k0, token[rt], (wr * RT + rt) * 16 + col < n_rows);
-          sees[rt] = w & live;
-        }
+        sees = att_window(P, seq, k0, token, col < n_rows) & live;
       }
+      f32x4_t sc[2];
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        f32x4_t sc[2];
+      for (int u = 0; u < 2; ++u) {
+        sc[u] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          sc[u] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int ks = 0; ks < KS; ++ks) sc[u] = mfma16<DT>(kf[u][ks], qf[ks], sc[u]);
+      }
+      float p[8];
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) sc[u] = mfma16<DT>(kf[u][ks], qf[rt][ks], sc[u]);
-        }
-        float p[8];
+      for (int x = 0; x < 8; ++x) p[x] = sc[x / 4][x % 4] * P.scale2;
+      if (masked) {
 #pragma unroll
-        for (int x = 0; x < 8; ++x) p[x] = sc[x / 4][x % 4] * P.scale2;
-        if (masked) {
+        for (int x = 0; x < 8; ++x)
+          if (!((sees >> (16 * (x / 4) + 4 * quarter + x % 4)) & 1u)) p[x] = -__builtin_inff();
+      }
+      float top = p[0];
 #pragma unroll
-          for (int x = 0; x < 8; ++x)
-            if (!((sees[rt] >> (16 * (x / 4) + 4 * quarter + x % 4)) & 1u)) p[x] = -__builtin_inff();
-        }
-        float top = p[0];
+      for (int x = 1; x < 8; ++x) top = fmaxf(top, p[x]);
+      top = quarters_max(top);
+      if (__any(top > m)) {
+        const float m_new = fmaxf(m, top);
+        const float a = m == -__builtin_inff() ? 0.0f : att_exp2(m - m_new);
+        m = m_new;
+        l *= a;
 #pragma unroll
-        for (int x = 1; x < 8; ++x) top = fmaxf(top, p[x]);
-        top = quarters_max(top);
-        if (__any(top > m[rt])) {
-          const float m_new = fmaxf(m[rt], top);
-          const float a = m[rt] == -__builtin_inff() ? 0.0f : att_exp2(m[rt] - m_new);
-          m[rt] = m_new;
-          l[rt] *= a;
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[f][i] *= a;
+      }
+      const float base = m == -__builtin_inff() ? 0.0f : m;     // (a row that has seen no key yet)
+      float sum = 0.0f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) { p[x] = att_exp2(p[x] - base); sum += p[x]; }
+      l += sum;
+      // the probabilities, at most 1, as the 16-bit operand of the second product: each is off by at most half a
+      // step of the type, which is what the output's own rounding is off by
+      const u32x4_t pf = {pack2<DT>(p[0], p[1]), pack2<DT>(p[2], p[3]), pack2<DT>(p[4], p[5]), pack2<DT>(p[6], p[7])};
+      if (!masked || !odd_v) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            u32x4_t vf;
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              vf[w] = __builtin_amdgcn_perm(vw[c][2 * w + 1][e / 2], vw[c][2 * w][e / 2], e % 2 ? 0x07060302u : 0x05040100u);
+            o[c * VE + e] = mfma16<DT>(vf, pf, o[c * VE + e]);
+          }
+      } else {
+        // 0 x infinity is no number: with such a value among the keys, every row adds up the keys that it sees, one by one
+#pragma unroll 1
+        for (int kk = 0; kk < 32; ++kk) {
+          if (!((live >> kk) & 1u)) continue;
+          const int x0 = 4 * (kk >> 4) + (kk & 3);
+          uint32_t w = pf[0];
+#pragma unroll
+          for (int x = 1; x < 4; ++x) w = (x0 >> 1) == x ? pf[x] : w;
+          const float mine = x0 & 1 ? hi_f32<DT>(w) : lo_f32<DT>(w);
+          const float pk = __shfl(mine, ((kk >> 2) & 3) * 16 + col, 64);
+          const bool see = (sees >> kk) & 1u;
+          const uint16_t *vr;
+          if constexpr (POW2) vr = reinterpret_cast<const uint16_t *>((kk < 16 ? vp[0] : vp[1]) + (kk & 15) * P.ldv);
+          else vr = reinterpret_cast<const uint16_t *>(vh + (uint64_t)(uint32_t)__shfl(slot, kk, 64) * P.ldv);
 #pragma unroll
           for (int f = 0; f < NF; ++f)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[rt][f][i] *= a;
-        }
-        const float base = m[rt] == -__builtin_inff() ? 0.0f : m[rt];     // (a row that has seen no key yet)
-        float sum = 0.0f;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) { p[x] = att_exp2(p[x] - base); sum += p[x]; }
-        l[rt] += sum;
-        // the probabilities, at most 1, as the 16-bit operand of the second product: each is off by at most half a
-        // step of the type, which is what the output's own rounding is off by
-        const u32x4_t pf = {pack2<DT>(p[0], p[1]), pack2<DT>(p[2], p[3]), pack2<DT>(p[4], p[5]), pack2<DT>(p[6], p[7])};
-        if (!masked || !odd_v) {
-#pragma unroll
-          for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-              u32x4_t vf;
-#pragma unroll
-              for (int w = 0; w < 4; ++w)
-                vf[w] = __builtin_amdgcn_perm(vw[c][2 * w + 1][e / 2], vw[c][2 * w][e / 2], e % 2 ? 0x07060302u : 0x05040100u);
-              o[rt][c * VE + e] = mfma16<DT>(vf, pf, o[rt][c * VE + e]);
+            for (int i = 0; i < 4; ++i) {
+              const int d = (f / VE) * 16 * VE + (quarter * 4 + i) * VE + f % VE;
+              if (see && (FULL || d < D)) o[f][i] += pk * cvt_in<DT>(vr[d]);
             }
-        } else {
-          // 0 x infinity is no number: with such a value among the keys, every row adds up the keys that it sees, one by one
-#pragma unroll 1
-          for (int kk = 0; kk < 32; ++kk) {
-            if (!((live >> kk) & 1u)) continue;
-            const int x0 = 4 * (kk >> 4) + (kk & 3);
-            uint32_t w = pf[0];
-#pragma unroll
-            for (int x = 1; x < 4; ++x) w = (x0 >> 1) == x ? pf[x] : w;
-            const float mine = x0 & 1 ? hi_f32<DT>(w) : lo_f32<DT>(w);
-            const float pk = __shfl(mine, ((kk >> 2) & 3) * 16 + col, 64);
-            const bool see = (sees[rt] >> kk) & 1u;
-            const uint16_t *vr;
-            if constexpr (POW2) vr = reinterpret_cast<const uint16_t *>((kk < 16 ? vp[0] : vp[1]) + (kk & 15) * P.ldv);
-            else vr = reinterpret_cast<const uint16_t *>(vh + (uint64_t)(uint32_t)__shfl(slot, kk, 64) * P.ldv);
-#pragma unroll
-            for (int f = 0; f < NF; ++f)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int d = (f / VE) * 16 * VE + (quarter * 4 + i) * VE + f % VE;
-                if (see && (FULL || d < D)) o[rt][f][i] += pk * cvt_in<DT>(vr[d]);
-              }
-          }
         }
       }
     }
@@ -448,56 +434,36 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
         if (d == 0) P.part_ml[which * ROWS + r] = make_float2(mm, ll);
       }
     };
+    const float lsum = quarters_sum(l);
+    __syncthreads();                                            // (the buffer's last readers are done)
+    if (quarter == 0) { merge_ml[(wave * 16 + col) * 2] = m; merge_ml[(wave * 16 + col) * 2 + 1] = lsum; }
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const float lsum = quarters_sum(l[rt]);
-      if constexpr (WK == 1) {
-        const int r = (wr * RT + rt) * 16 + col;
-        if (r < n_rows) {
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
-          for (int c = 0; c < NC; ++c)
+      for (int i = 0; i < 4; ++i) {
+        float *mp = merge_o + (wave * 16 + col) * OP + c * 16 * VE + (quarter * 4 + i) * VE;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int d = c * 16 * VE + (quarter * 4 + i) * VE;
-              float x[VE];
-#pragma unroll
-              for (int e = 0; e < VE; ++e) x[e] = o[rt][c * VE + e][i];
-              if (FULL || d < D) store_row(r, d, x, m[rt], lsum);
-            }
-        }
-      } else {
-        static_assert(WK == 1 || WR == 1, "the merge buffer is that of one row group");
-        __syncthreads();                                            // (the buffer's last readers are done)
-        if (quarter == 0) { merge_ml[(wk * 16 + col) * 2] = m[rt]; merge_ml[(wk * 16 + col) * 2 + 1] = lsum; }
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float *mp = merge_o + (wk * 16 + col) * OP + c * 16 * VE + (quarter * 4 + i) * VE;
-#pragma unroll
-            for (int e = 0; e < VE; e += 4)
-              *reinterpret_cast<f32x4_t *>(mp + e) = f32x4_t{o[rt][c * VE + e][i], o[rt][c * VE + e + 1][i], o[rt][c * VE + e + 2][i], o[rt][c * VE + e + 3][i]};
-          }
-        __syncthreads();
-        for (int x = tid; x < 16 * (DP / VE); x += ATT_THREADS) {
-          const int rr = x / (DP / VE), d = (x - rr * (DP / VE)) * VE, r = rt * 16 + rr;
-          if (r >= n_rows || (!FULL && d >= D)) continue;
-          float mm = merge_ml[rr * 2], ll = 0.0f, y[VE];
-#pragma unroll
-          for (int w = 1; w < WK; ++w) mm = fmaxf(mm, merge_ml[(w * 16 + rr) * 2]);
-#pragma unroll
-          for (int e = 0; e < VE; ++e) y[e] = 0.0f;
-#pragma unroll
-          for (int w = 0; w < WK; ++w) {
-            // (a part without any key has l = 0 and O = 0, or, where all its scores were no numbers, neither: kept as it is)
-            const float mw = merge_ml[(w * 16 + rr) * 2], a = mw == -__builtin_inff() ? 1.0f : att_exp2(mw - mm);
-            ll += a * merge_ml[(w * 16 + rr) * 2 + 1];
-#pragma unroll
-            for (int e = 0; e < VE; ++e) y[e] += a * merge_o[(w * 16 + rr) * OP + d + e];
-          }
-          store_row(r, d, y, mm, ll);
-        }
+        for (int e = 0; e < VE; e += 4)
+          *reinterpret_cast<f32x4_t *>(mp + e) = f32x4_t{o[c * VE + e][i], o[c * VE + e + 1][i], o[c * VE + e + 2][i], o[c * VE + e + 3][i]};
       }
+    __syncthreads();
+    for (int x = tid; x < 16 * (DP / VE); x += ATT_THREADS) {
+      const int rr = x / (DP / VE), d = (x - rr * (DP / VE)) * VE;
+      if (rr >= n_rows || (!FULL && d >= D)) continue;
+      float mm = merge_ml[rr * 2], ll = 0.0f, y[VE];
+#pragma unroll
+      for (int w = 1; w < WK; ++w) mm = fmaxf(mm, merge_ml[(w * 16 + rr) * 2]);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) y[e] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WK; ++w) {
+        // (a part without any key has l = 0 and O = 0, or, where all its scores were no numbers, neither: kept as it is)
+        const float mw = merge_ml[(w * 16 + rr) * 2], a = mw == -__builtin_inff() ? 1.0f : att_exp2(mw - mm);
+        ll += a * merge_ml[(w * 16 + rr) * 2 + 1];
+#pragma unroll
+        for (int e = 0; e < VE; ++e) y[e] += a * merge_o[(w * 16 + rr) * OP + d + e];
+      }
+      store_row(rr, d, y, mm, ll);
     }
     if (!whole && u0 == 0 && tid == 0) P.joins[share] = make_int4(s, h, tile, run.sharers());
   } while (run.next(P));
@@ -926,7 +892,8 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
 
 // Joins the partial results of the tiles of rows whose keys several workgroups had: workgroup b takes the tile
 // that begins in share b, whose other parts are the first of the shares after it, sixteen rows of it per workgroup.  Threads: (group of parts) x
-// (row, 4 features); the groups' sums are joined in LDS in a fixed order.
+// (row, 4 features); the groups' sums are joined in LDS in a fixed order.  5 to 6 us for tiles of 16 rows, most of it a launch's and
+// a dependent chain's; 19 us for the 256-row tiles of 16 sequences (one workgroup per tile took 45).
 template <int ROWS> constexpr int JOIN_THREADS = ROWS == 16 ? 1024 : 256;
 template <int DT, int DP, int ROWS>
 __global__ __launch_bounds__(JOIN_THREADS<ROWS>) void tree_attention_join_kernel(const AttParams P) {
