@@ -477,10 +477,12 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
 // operand), then cover all banks.  V needs no permutes here, and its features keep their order: block f of the
 // output is 16 f .. 16 f + 15.
 //
-// Measured (64 drafted tokens x 16 sequences of up to 16384 keys, 8 key heads of 128, fp16): 350 us a call, 4280 cycles for
+// Measured (64 drafted tokens x 16 sequences of up to 16384 keys, 8 key heads of 128, fp16): 341 us a call, about 4200 cycles for
 // 64 keys and 256 rows, of which 2176 are matrix instructions (two wavefronts per SIMD) and 2048 the LDS reads of
-// all eight wavefronts at the full rate; 2 x 2048 prompt tokens on up to 6000 cached, 32 heads, bf16: 433 us = 799 TFLOP/s.
-// Under such calls the clock falls to its power limit.  Four wavefronts of 64 rows read half as much from LDS, but one
+// all eight wavefronts at the full rate; 2 x 2048 prompt tokens on up to 6000 cached, 32 heads, bf16: 419 us = 826 TFLOP/s.
+// Under such calls the clock falls to its power limit (half of the wavefronts asleep for 640 cycles of every stage cost nothing), so
+// fewer instructions count for more than a better overlap: one look at a table's entry per wavefront where all keys of a stage
+// exist, instead of one per lane, 433 -> 419.  Four wavefronts of 64 rows read half as much from LDS, but one
 // wavefront per SIMD has nothing to run beside its own vector instructions: 5500 cycles.
 //
 // The scores of the 32 keys after are multiplied while those of these are turned into probabilities, and
@@ -611,21 +613,48 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
     const char *kh = reinterpret_cast<const char *>(P.k + (long long)h * D), *vh = reinterpret_cast<const char *>(P.v + (long long)h * D);
 
     // The blocks of the keys to be loaded are read from the table ahead, IDS at a time, into LDS: a wait for a list in
-    // memory would be one for the rows in flight too.  Every wavefront calls this, between barriers.
+    // memory would be one for the rows in flight too.  Every wavefront calls this, between barriers.  clean: all blocks
+    // so far exist.
     int page0 = 0;
+    bool clean = true;
     auto fetch_ids = [&](int k0) {
       page0 = k0 / P.block_tokens;
       const int last = (keys_end - 1) / P.block_tokens;
-      for (int x = tid; x < C::IDS; x += THREADS) ids[x] = table[page0 + x < last ? page0 + x : last];
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
+      bool bad = false;
+      for (int x = tid; x < C::IDS; x += THREADS) {
+        const int id = table[page0 + x < last ? page0 + x : last];
+        bad |= id < 0 || id >= P.n_pool_blocks;
+        ids[x] = id;
+      }
+      if constexpr (FULL && POW2) {
+        if (__syncthreads_or(bad)) clean = false;
+      } else {
+        __syncthreads();
+      }
     };
     // The wavefront's rows of K and of V of the stage of keys from k0 on into place b of the ring: 2 NL load instructions,
     // whatever keys there are, so that the waits below can count them.  Keys that do not exist are rows of zeros.
     // Returns the keys that exist.
     auto issue = [&](int b, int k0) -> uint64_t {
       unsigned char *kb = att_smem + b * 2 * BUF + wave * WROWS * ROWB, *vb = kb + BUF;
+      int ln = lane;                             // (the few instructions anew each time: kept through the loop they cost registers)
+      // piece at place ln % CH of row ln / CH + RPI i of the wavefront's, which is row (WROWS wave + that) of the stage
+      auto row_of = [&](int i) { return ln / CH + RPI * i; };
+      auto piece_of = [&](int i) { return (uint32_t)((ln % CH) ^ ((WROWS * wave + row_of(i)) & SW)); };
+      if (FULL && POW2 && clean && k0 + STAGE <= keys_end) {
+        // nearly always: the wavefront's rows lie in one block, and every key of the stage exists
+        asm volatile("" : "+v"(ln));
+        const int kw = k0 + WROWS * wave;
+        const int id = __builtin_amdgcn_readfirstlane(ids[(kw >> P.block_shift) - page0]);
+        const uint64_t row0 = (uint32_t)((id << P.block_shift) + (kw & (P.block_tokens - 1)));
+        const char *kr = kh + row0 * P.ldk, *vr = vh + row0 * P.ldv;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          load_to_lds(kr, row_of(i) * P.ldk + piece_of(i) * 16, kb + i * 1024);
+          load_to_lds(vr, row_of(i) * P.ldv + piece_of(i) * 16, vb + i * 1024);
+        }
+        return STAGE == 64 ? ~0ull : 0xffffffffull;
+      }
       const int kk = k0 + (lane & (STAGE - 1)), ke = kk < keys_end ? kk : keys_end - 1;
       const int page = POW2 ? ke >> P.block_shift : ke / P.block_tokens, off = POW2 ? ke & (P.block_tokens - 1) : ke - page * P.block_tokens;
       const int id = ids[page > page0 ? page - page0 : 0];         // (behind the last stage nothing is read ahead)
@@ -635,42 +664,23 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
       const int slot = ok ? (POW2 ? (id << P.block_shift) + off : id * P.block_tokens + off) : 0;
       const uint32_t here = (uint32_t)(live >> (WROWS * wave)) & ((1u << WROWS) - 1u);
       const uint64_t row0 = (uint32_t)__builtin_amdgcn_readlane(slot, WROWS * wave);
-      const char *k0p = kh + row0 * P.ldk, *v0p = vh + row0 * P.ldv;
-      int ln = lane;
-      asm volatile("" : "+v"(ln));               // (the few instructions anew each time: kept through the loop they cost registers)
-      const int lrow = ln / CH, lpos = ln % CH;
-      auto load = [&](int i, bool all) {
-        // row lrow + RPI i of the wavefront's, row (WROWS wave + that) of the stage: its piece at place lpos
-        const int r = lrow + RPI * i;
-        const uint32_t piece = (uint32_t)(lpos ^ ((WROWS * wave + r) & SW));
+      asm volatile("" : "+v"(ln));
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int r = row_of(i);
+        const uint32_t piece = piece_of(i);
         const char *kr, *vr;
         if constexpr (POW2) {
-          if (all) {
-            load_to_lds(k0p, r * P.ldk + piece * 16, kb + i * 1024);
-            load_to_lds(v0p, r * P.ldv + piece * 16, vb + i * 1024);
-            return;
-          }
-          kr = k0p + (r * P.ldk + piece * 16);
-          vr = v0p + (r * P.ldv + piece * 16);
+          kr = kh + row0 * P.ldk + (r * P.ldk + piece * 16);
+          vr = vh + row0 * P.ldv + (r * P.ldv + piece * 16);
         } else {
           const uint64_t row = (uint32_t)__shfl(slot, WROWS * wave + r, 64);
           kr = kh + row * P.ldk + piece * 16;
           vr = vh + row * P.ldv + piece * 16;
         }
-        if (!all) {
-          const bool there = ((here >> r) & 1u) && (FULL || (int)piece * 8 < D);
-          kr = there ? kr : reinterpret_cast<const char *>(&att_zeros);
-          vr = there ? vr : reinterpret_cast<const char *>(&att_zeros);
-        }
-        load_to_lds(kr, kb + i * 1024);
-        load_to_lds(vr, vb + i * 1024);
-      };
-      if (FULL && here == (1u << WROWS) - 1u) {
-#pragma unroll
-        for (int i = 0; i < NL; ++i) load(i, true);
-      } else {
-#pragma unroll
-        for (int i = 0; i < NL; ++i) load(i, false);
+        const bool there = ((here >> r) & 1u) && (FULL || (int)piece * 8 < D);
+        load_to_lds(there ? kr : reinterpret_cast<const char *>(&att_zeros), kb + i * 1024);
+        load_to_lds(there ? vr : reinterpret_cast<const char *>(&att_zeros), vb + i * 1024);
       }
       return live;
     };
