@@ -479,10 +479,10 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
 //
 // Measured (64 drafted tokens x 16 sequences of up to 16384 keys, 8 key heads of 128, fp16): 341 us a call, about 4200 cycles for
 // 64 keys and 256 rows, of which 2176 are matrix instructions (two wavefronts per SIMD) and 2048 the LDS reads of
-// all eight wavefronts at the full rate; 2 x 2048 prompt tokens on up to 6000 cached, 32 heads, bf16: 419 us = 826 TFLOP/s.
+// all eight wavefronts at the full rate; 2 x 2048 prompt tokens on up to 6000 cached, 32 heads, bf16: 411 us = 842 TFLOP/s.
 // Under such calls the clock falls to its power limit (half of the wavefronts asleep for 640 cycles of every stage cost nothing), so
 // fewer instructions count for more than a better overlap: one look at a table's entry per wavefront where all keys of a stage
-// exist, instead of one per lane, 433 -> 419.  Four wavefronts of 64 rows read half as much from LDS, but one
+// exist, instead of one per lane, 433 -> 419, the reference kept as it is used, 411.  Four wavefronts of 64 rows read half as much from LDS, but one
 // wavefront per SIMD has nothing to run beside its own vector instructions: 5500 cycles.
 //
 // The scores of the 32 keys after are multiplied while those of these are turned into probabilities, and
@@ -559,7 +559,7 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
   constexpr int RPI = 64 / CH, NL = WROWS / RPI; // rows of one load instruction, load instructions
   constexpr int HALVES = STAGE / 32;
   constexpr int BUF = STAGE * ROWB;              // bytes of K (of V) of a stage
-  constexpr float REF = DT == DT_F16 ? 0.0f : 16.0f;
+  constexpr float REF = DT == DT_F16 ? 0.0f : 16.0f, NONE = 1.0e30f;
   constexpr uint32_t ONES = DT == DT_F16 ? 0x3c003c00u : 0x3f803f80u;
   static_assert(NL * RPI == WROWS, "whole load instructions");
   extern __shared__ __attribute__((aligned(16))) unsigned char att_smem[];       // [RING][K, V][STAGE][ROWB], [IDS]
@@ -600,10 +600,10 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
       }
     }
     f32x4_t o[RT][NF], l[RT];
-    float m[RT];
+    float ref[RT];                               // -m; NONE where a row has seen no key yet: any score but minus infinity then makes an infinity
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      m[rt] = -__builtin_inff(); l[rt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+      ref[rt] = NONE; l[rt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int f = 0; f < NF; ++f) o[rt][f] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     }
@@ -775,11 +775,9 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
         auto probabilities = [&](const f32x4_t (&x)[RT][2], int u) {
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
-            // (a row that has seen no key yet: any score but minus infinity then makes an infinity)
-            const float ref = m[rt] == -__builtin_inff() ? 1.0e30f : -m[rt];
             float p[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = att_exp2(fmaf(x[rt][u][i], P.scale2, ref));
+            for (int i = 0; i < 4; ++i) p[i] = att_exp2(fmaf(x[rt][u][i], P.scale2, ref[rt]));
             const uint32_t lo = pack2<DT>(p[0], p[1]), hi = pack2<DT>(p[2], p[3]);
             pf[rt][2 * u] = lo; pf[rt][2 * u + 1] = hi;
             any = att_larger<DT>(any, lo, hi);
@@ -808,9 +806,10 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
             for (int u = 0; u < 2; ++u)
 #pragma unroll
               for (int i = 0; i < 4; ++i) top = fmaxf(top, x[rt][u][i]);
-            const float m_new = fmaxf(m[rt], quarters_max(top) * P.scale2 + REF);
-            const float a = m[rt] == -__builtin_inff() ? 0.0f : att_exp2(m[rt] - m_new);
-            m[rt] = m_new;
+            top = quarters_max(top) * P.scale2 + REF;
+            const float ref_new = top == -__builtin_inff() ? ref[rt] : fminf(ref[rt], -top);
+            const float a = att_exp2(ref_new - ref[rt]);       // (0 from NONE on)
+            ref[rt] = ref_new;
 #pragma unroll
             for (int i = 0; i < 4; ++i) l[rt][i] *= a;
 #pragma unroll
@@ -892,7 +891,7 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
         float *pp = P.part + (which * ROWS + r) * DP + 4 * quarter;
 #pragma unroll
         for (int f = 0; f < NF; ++f) *reinterpret_cast<f32x4_t *>(pp + 16 * f) = o[rt][f];
-        if (quarter == 0) P.part_ml[which * ROWS + r] = make_float2(m[rt], ll);
+        if (quarter == 0) P.part_ml[which * ROWS + r] = make_float2(ref[rt] == NONE ? -__builtin_inff() : -ref[rt], ll);
       }
     }
     if (!whole && u0 == 0 && tid == 0) P.joins[share] = make_int4(s, h, tile, run.sharers());
