@@ -901,8 +901,9 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
 
 // Joins the partial results of the tiles of rows whose keys several workgroups had: workgroup b takes the tile
 // that begins in share b, whose other parts are the first of the shares after it, sixteen rows of it per workgroup.  Threads: (group of parts) x
-// (row, 4 features); the groups' sums are joined in LDS in a fixed order.  5 to 6 us for tiles of 16 rows, most of it a launch's and
-// a dependent chain's; 19 us for the 256-row tiles of 16 sequences (one workgroup per tile took 45).
+// (row, 4 features); the groups' sums are joined in LDS in a fixed order.  4 us for tiles of 16 rows, a launch's and a
+// dependent chain's (6 with one load after the other); 19 us for the 256-row tiles of 16 sequences, whose parts are some 60 MB written and
+// read (one workgroup per tile took 45).
 template <int ROWS> constexpr int JOIN_THREADS = ROWS == 16 ? 1024 : 256;
 template <int DT, int DP, int ROWS>
 __global__ __launch_bounds__(JOIN_THREADS<ROWS>) void tree_attention_join_kernel(const AttParams P) {
@@ -910,7 +911,7 @@ __global__ __launch_bounds__(JOIN_THREADS<ROWS>) void tree_attention_join_kernel
   const int4 job = P.joins[share];
   if (job.x < 0) return;
   constexpr int THREADS = JOIN_THREADS<ROWS>, QUADS = DP / 4, ITEMS = 16 * QUADS;
-  constexpr int SETS = ITEMS < THREADS ? THREADS / ITEMS : 1;
+  constexpr int SETS = ITEMS < THREADS ? THREADS / ITEMS : 1, AHEAD = 4;
   __shared__ __attribute__((aligned(16))) float sum_o[SETS > 1 ? SETS * 16 * DP : 4];
   __shared__ float sum_l[SETS > 1 ? SETS * 16 : 1];
   const AttSeq seq = att_seq(P, job.x);
@@ -924,14 +925,31 @@ __global__ __launch_bounds__(JOIN_THREADS<ROWS>) void tree_attention_join_kernel
     float mm = -__builtin_inff(), ll = 0.0f;
     f32x4_t y = {0.0f, 0.0f, 0.0f, 0.0f};
     if (r < n_rows) {
-      for (int i = 0; i < parts; ++i) mm = fmaxf(mm, P.part_ml[part_at(i, r)].x);
-      for (int i = set; i < parts; i += SETS) {
-        const float2 ml = P.part_ml[part_at(i, r)];
-        const float a = ml.x == -__builtin_inff() ? 1.0f : att_exp2(ml.x - mm);
-        ll += a * ml.y;
-        const f32x4_t z = *reinterpret_cast<const f32x4_t *>(P.part + part_at(i, r) * DP + d);
+      // (AHEAD loads side by side: the last part stands in for those behind it, and is not added)
+      for (int i0 = 0; i0 < parts; i0 += 2 * AHEAD) {
+        float x[2 * AHEAD];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] += a * z[e];
+        for (int i = 0; i < 2 * AHEAD; ++i) x[i] = P.part_ml[part_at(i0 + i < parts ? i0 + i : parts - 1, r)].x;
+#pragma unroll
+        for (int i = 0; i < 2 * AHEAD; ++i) mm = fmaxf(mm, x[i]);
+      }
+      for (int i0 = set; i0 < parts; i0 += SETS * AHEAD) {
+        float2 ml[AHEAD];
+        f32x4_t z[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          const long long at = part_at(i0 + SETS * i < parts ? i0 + SETS * i : parts - 1, r);
+          ml[i] = P.part_ml[at];
+          z[i] = *reinterpret_cast<const f32x4_t *>(P.part + at * DP + d);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          if (i0 + SETS * i >= parts) continue;
+          const float a = ml[i].x == -__builtin_inff() ? 1.0f : att_exp2(ml[i].x - mm);
+          ll += a * ml[i].y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] += a * z[i][e];
+        }
       }
     }
     if constexpr (SETS > 1) {
