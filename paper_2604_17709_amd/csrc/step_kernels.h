@@ -16,7 +16,7 @@ constexpr int STEP_THREADS = 1024;
 constexpr int STEP_MAX_SEQS = 8192;
 constexpr int STEP_ROWS = 4;                     // consecutive rows of one thread: one bisection, 16-byte stores
 
-// inclusive sum over the workgroup's threads; total: the sum of all.  scratch: STEP_THREADS / 64 values
+// inclusive sum over the workgroup's STEP_THREADS threads; total: the sum of all.  scratch: STEP_THREADS / 64 values
 template <typename TV> __device__ __forceinline__ TV block_scan(TV v, TV *scratch, TV *total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
@@ -28,7 +28,8 @@ template <typename TV> __device__ __forceinline__ TV block_scan(TV v, TV *scratc
   if (lane == 63) scratch[wave] = v;
   __syncthreads();
   TV before = 0, all = 0;
-  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) {
+#pragma unroll
+  for (int w = 0; w < STEP_THREADS / 64; ++w) {    // (reads side by side: one after the other they cost 0.3 us a sum)
     const TV u = scratch[w];
     if (w < wave) before += u;
     all += u;
@@ -59,7 +60,7 @@ struct KvStepParams {
 // ceil(c / b) .. ceil((c + m) / b) - 1 are new; the new blocks of all sequences, counted in order, take
 // the free list's entries in order.  Entries of the table below ceil(c / b) are read, those from there
 // on are written, so no workgroup reads what another writes; a new block is written by the row of
-// its first token.  8 us for 8 sequences (a call takes the host 11.5), 13.5 for 2048 sequences and 8000 rows.
+// its first token.  7.4 us for 8 sequences (a call takes the host 11.5), 12.6 for 2048 sequences and 8000 rows.
 __global__ __launch_bounds__(STEP_THREADS) void kv_step_kernel(const KvStepParams P) {
   __shared__ int row_start[STEP_MAX_SEQS + 1];
   __shared__ int need_start[STEP_MAX_SEQS + 1];
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(STEP_THREADS) void kv_step_kernel(const KvStepParam
 // ---- the plan of the compacting copy --------------------------------------------------------------
 constexpr int PLAN_IDS = 2;                                   // consecutive blocks of the walk per thread
 constexpr int PLAN_CHUNK = STEP_THREADS * PLAN_IDS;           // blocks of the walk per workgroup
-constexpr int PLAN_AHEAD = 8;                                 // blocks per thread that are looked up together where they are only counted
+constexpr int PLAN_AHEAD = 16;                                // blocks per thread that are looked up together where they are only counted
 enum { KV_PLAN_BAD_BLOCK = 1, KV_PLAN_BUFFER_FULL = 2, KV_PLAN_TABLE_FULL = 4, KV_PLAN_RUNS_FULL = 8 };
 
 struct KvPlanParams {
@@ -165,8 +166,8 @@ struct KvPlanParams {
 // the block before it.  Workgroups 0 .. n_chunks - 1 write the runs of PLAN_CHUNK blocks each; the number
 // of runs before its chunk a workgroup counts by itself, in one pass over the ids of the earlier blocks: PLAN_AHEAD
 // look-ups of a thread go on side by side (a bisection in LDS, two loads), and there is one sum at the end.
-// The other workgroups write the remapped table and the positions.  7.7 us for 16 sequences of 32 blocks; 33 us for 1024 sequences
-// and 66000 blocks, of which 18 are the last workgroup's count and 4 the words behind the last run.
+// The other workgroups write the remapped table and the positions.  7 us for 16 sequences of 32 blocks; 30 us for 1024 sequences
+// and 66000 blocks, of which half is the last workgroup's count.
 __global__ __launch_bounds__(STEP_THREADS) void kv_plan_kernel(const KvPlanParams P) {
   __shared__ int start[STEP_MAX_SEQS + 1];                    // first block of the walk of every sequence
   __shared__ long long scratch64[STEP_THREADS / 64];
@@ -312,7 +313,14 @@ __global__ __launch_bounds__(STEP_THREADS) void kv_plan_kernel(const KvPlanParam
         P.plan[0] = any ? 0 : runs; P.plan[1] = any ? 0 : nb;
         P.plan[2] = any; P.plan[3] = 0;
       }
-      for (long long i = (runs < P.capacity ? runs : P.capacity) * 3LL + tid; i < 3 * P.capacity; i += STEP_THREADS) P.plan[KV_PLAN_HEADER + i] = 0;
+      // the words behind the last run: zeros, 16 bytes at a time where they lie that way
+      int *words = P.plan + KV_PLAN_HEADER;
+      const long long from = (runs < P.capacity ? runs : P.capacity) * 3LL, end = 3 * P.capacity;
+      long long wide = (reinterpret_cast<uintptr_t>(words) & 15) == 0 ? (from + 3) & ~3LL : end;
+      wide = wide < end ? wide : end;
+      for (long long i = from + tid; i < wide; i += STEP_THREADS) words[i] = 0;
+      for (long long i = wide + 4LL * tid; i + 4 <= end; i += 4LL * STEP_THREADS) *reinterpret_cast<int4 *>(words + i) = make_int4(0, 0, 0, 0);
+      for (long long i = wide + ((end - wide) & ~3LL) + tid; i < end; i += STEP_THREADS) words[i] = 0;
     }
     return;
   }

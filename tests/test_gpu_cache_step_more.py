@@ -75,3 +75,20 @@ def test_outputs_that_a_step_allocates(dn, n, rows):
     assert [tuple(t.shape) for t in got] == [(n + 1,), (rows,), (rows,), (4,)]
     assert all(torch.equal(g, w) for g, w in zip(got, want)) and torch.equal(*tables)
     assert got.slots.data_ptr() % 16 == 0 and got.positions.data_ptr() % 16 == 0
+
+
+@pytest.mark.parametrize("shift", [0, 1, 2, 3])
+@pytest.mark.parametrize("spare", [0, 1, 2, 5])
+def test_plan_at_any_word(dn, shift, spare):
+    """The plan may begin at any word: every word of it is written, none beside it."""
+    import torch
+    counts = [30, 0, 11]
+    table, n_pool = walk(9, counts, 4)
+    want = dn.deinfer_kv_compact_plan(table, np.array(counts), n_pool, 41 + spare, 2)
+    n = len(want[0])
+    room = torch.full((n + 8,), 55, dtype=torch.int32, device="cuda")
+    out = (room[shift:shift + n], torch.zeros(table.shape, dtype=torch.int32, device="cuda"), torch.zeros((41 + spare) * 2, dtype=torch.int32, device="cuda"))
+    got = dn.deinfer_kv_compact_plan_device(ints(table), ints(np.array(counts) * 2), n_pool, 41 + spare, 2, out=out)
+    for g, w in zip(got, want):
+        assert np.array_equal(host(g), w)
+    assert bool((room[:shift] == 55).all()) and bool((room[shift + n:] == 55).all())
