@@ -479,10 +479,10 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
 //
 // Measured (64 drafted tokens x 16 sequences of up to 16384 keys, 8 key heads of 128, fp16): 341 us a call, about 4200 cycles for
 // 64 keys and 256 rows, of which 2176 are matrix instructions (two wavefronts per SIMD) and 2048 the LDS reads of
-// all eight wavefronts at the full rate; 2 x 2048 prompt tokens on up to 6000 cached, 32 heads, bf16: 411 us = 842 TFLOP/s.
+// all eight wavefronts at the full rate; 2 x 2048 prompt tokens on up to 6000 cached, 32 heads, bf16: 415 us = 834 TFLOP/s.
 // Under such calls the clock falls to its power limit (half of the wavefronts asleep for 640 cycles of every stage cost nothing), so
 // fewer instructions count for more than a better overlap: one look at a table's entry per wavefront where all keys of a stage
-// exist, instead of one per lane, 433 -> 419, the reference kept as it is used, 411.  Four wavefronts of 64 rows read half as much from LDS, but one
+// exist, instead of one per lane, 433 -> 419, the reference kept as it is used, 411 to 416.  Four wavefronts of 64 rows read half as much from LDS, but one
 // wavefront per SIMD has nothing to run beside its own vector instructions: 5500 cycles.
 //
 // The scores of the 32 keys after are multiplied while those of these are turned into probabilities, and
@@ -529,12 +529,21 @@ __device__ __forceinline__ void load_to_lds(const void *from, void *to) {
   (void)from; (void)to;
 #endif
 }
-// the same with an address that is the wavefront's and a lane's offset
+// the same with an address that is the wavefront's (see settled) and a lane's offset
 __device__ __forceinline__ void load_to_lds(const void *from, uint32_t offset, void *to) {
 #if defined(__HIP_DEVICE_COMPILE__)
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_at(to)), "v"(offset), "s"(from) : "memory", "m0");
 #else
   (void)from; (void)offset; (void)to;
+#endif
+}
+// Five wait states, after which a lane's value that was read into scalar registers right before may be a load's address: the
+// compiler keeps them for its own loads, and does not see into the asm.
+__device__ __forceinline__ void settled(const char *&a, const char *&b) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_nop 4" : "+s"(a), "+s"(b));
+#else
+  (void)a; (void)b;
 #endif
 }
 // Lanes 4 r + c of sixteen address 8 bytes (columns 4 c .. 4 c + 3) of row r < 4; lane j gets column j of the four rows.
@@ -648,6 +657,7 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
         const int id = __builtin_amdgcn_readfirstlane(ids[(kw >> P.block_shift) - page0]);
         const uint64_t row0 = (uint32_t)((id << P.block_shift) + (kw & (P.block_tokens - 1)));
         const char *kr = kh + row0 * P.ldk, *vr = vh + row0 * P.ldv;
+        settled(kr, vr);
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
           load_to_lds(kr, row_of(i) * P.ldk + piece_of(i) * 16, kb + i * 1024);
@@ -902,7 +912,7 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
 // Joins the partial results of the tiles of rows whose keys several workgroups had: workgroup b takes the tile
 // that begins in share b, whose other parts are the first of the shares after it, sixteen rows of it per workgroup.  Threads: (group of parts) x
 // (row, 4 features); the groups' sums are joined in LDS in a fixed order.  4 us for tiles of 16 rows, a launch's and a
-// dependent chain's (6 with one load after the other); 19 us for the 256-row tiles of 16 sequences, whose parts are some 60 MB written and
+// dependent chain's (6 with one load after the other); 18 us for the 256-row tiles of 16 sequences, whose parts are some 60 MB written and
 // read (one workgroup per tile took 45).
 template <int ROWS> constexpr int JOIN_THREADS = ROWS == 16 ? 1024 : 256;
 template <int DT, int DP, int ROWS>
@@ -911,7 +921,7 @@ __global__ __launch_bounds__(JOIN_THREADS<ROWS>) void tree_attention_join_kernel
   const int4 job = P.joins[share];
   if (job.x < 0) return;
   constexpr int THREADS = JOIN_THREADS<ROWS>, QUADS = DP / 4, ITEMS = 16 * QUADS;
-  constexpr int SETS = ITEMS < THREADS ? THREADS / ITEMS : 1, AHEAD = 4;
+  constexpr int SETS = ITEMS < THREADS ? THREADS / ITEMS : 1, AHEAD = ROWS == 16 ? 4 : 2;      // (large tiles have few parts)
   __shared__ __attribute__((aligned(16))) float sum_o[SETS > 1 ? SETS * 16 * DP : 4];
   __shared__ float sum_l[SETS > 1 ? SETS * 16 : 1];
   const AttSeq seq = att_seq(P, job.x);
