@@ -477,9 +477,9 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
 // operand), then cover all banks.  V needs no permutes here, and its features keep their order: block f of the
 // output is 16 f .. 16 f + 15.
 //
-// Measured (64 drafted tokens x 16 sequences of up to 16384 keys, 8 key heads of 128, fp16): 341 us a call, about 4200 cycles for
+// Measured (64 drafted tokens x 16 sequences of up to 16384 keys, 8 key heads of 128, fp16): 339 us a call, about 4200 cycles for
 // 64 keys and 256 rows, of which 2176 are matrix instructions (two wavefronts per SIMD) and 2048 the LDS reads of
-// all eight wavefronts at the full rate; 2 x 2048 prompt tokens on up to 6000 cached, 32 heads, bf16: 415 us = 834 TFLOP/s.
+// all eight wavefronts at the full rate; 2 x 2048 prompt tokens on up to 6000 cached, 32 heads, bf16: 417 us = 829 TFLOP/s.
 // Under such calls the clock falls to its power limit (half of the wavefronts asleep for 640 cycles of every stage cost nothing), so
 // fewer instructions count for more than a better overlap: one look at a table's entry per wavefront where all keys of a stage
 // exist, instead of one per lane, 433 -> 419, the reference kept as it is used, 411 to 416.  Four wavefronts of 64 rows read half as much from LDS, but one
