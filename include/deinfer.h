@@ -435,7 +435,8 @@ int deinfer_rope_store(const void *q, int64_t ldq, int64_t n_q_heads,
  *   block_tokens) entries of a row in use.  dtype: bf16 or fp16.  head_dim: a multiple of 8, at most 256.  scale: a normal
  *   positive number of fp32, with 1 / ln 2 on it too.
  *   q, pools and out 16-byte aligned, pitches multiples of 8.  out must not overlap q.
- * Scores, maxima, sums and outputs are fp32; the probabilities are rounded to the storage type for the second product, the
+ * Scores, maxima, sums and outputs are fp32; the probabilities are rounded to the storage type for the second product (off by
+ * half a step each; in fp16 those under 2^-26 of a row's largest by up to 2^-37 of that), their sum is that of the rounded ones, the
  * output is rounded once.  Results do not depend on timing.  The workspace (deinfer_tree_attention_workspace_bytes,
  * host only; 256-byte aligned) needs no clearing and serves one call at a time.  Its size is that of the call's own T
  * and n_seqs: more rows need no less, fewer sequences with the same rows may need more.  T <= 2^28, T n_q_heads < 2^30,

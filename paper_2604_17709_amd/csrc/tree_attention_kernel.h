@@ -173,14 +173,10 @@ template <int ROWS, int UNIT, int THREADS> struct AttRun {
 };
 
 __device__ __forceinline__ float att_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
-// the larger (the sum) of the four quarters of the wave, in every lane
+// the largest of the four quarters of the wave, in every lane
 __device__ __forceinline__ float quarters_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16, 64));
   return fmaxf(x, __shfl_xor(x, 32, 64));
-}
-__device__ __forceinline__ float quarters_sum(float x) {
-  x += __shfl_xor(x, 16, 64);
-  return x + __shfl_xor(x, 32, 64);
 }
 
 // Bits of the 32 keys from k0 on that row `token` of the sequence sees among the drafted ones (all ones for cached keys).
@@ -220,6 +216,10 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
   constexpr int NF = NC * VE;                    // 16-feature blocks of the output
   constexpr int VW = VE / 2;                     // words of a piece
   constexpr int OP = DP + 4;                     // row pitch of the merge buffer in LDS
+  // The largest probability of a row: fp16's smallest normal number is 2^-14, and what lies below it has fewer bits and is
+  // nothing from 2^-25 on, which a long tail of keys may add up to a good part of the output.  O and l have the factor alike.
+  constexpr float LIFT = DT == DT_F16 ? 32768.0f : 1.0f;
+  constexpr uint32_t ONES = DT == DT_F16 ? 0x3c003c00u : 0x3f803f80u;
   __shared__ __attribute__((aligned(16))) float merge_o[WK * 16 * OP];
   __shared__ float merge_ml[2 * WK * 16];
   __shared__ long long scan[ATT_THREADS / 64];
@@ -248,8 +248,9 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
         if (col < n_rows && (FULL || ks * 32 + quarter * 8 < D)) qf[ks] = *reinterpret_cast<const u32x4_t *>(qp + ks * 32);
       }
     }
-    f32x4_t o[NF];
-    float m = -__builtin_inff(), l = 0.0f;
+    f32x4_t o[NF], l = {0.0f, 0.0f, 0.0f, 0.0f};
+    float m = -__builtin_inff();
+    const u32x4_t ones = {ONES, ONES, ONES, ONES};
 #pragma unroll
     for (int f = 0; f < NF; ++f) o[f] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     // keys that some row may see, and keys that every row sees
@@ -363,20 +364,21 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
         const float m_new = fmaxf(m, top);
         const float a = m == -__builtin_inff() ? 0.0f : att_exp2(m - m_new);
         m = m_new;
-        l *= a;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) l[i] *= a;
 #pragma unroll
         for (int f = 0; f < NF; ++f)
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[f][i] *= a;
       }
       const float base = m == -__builtin_inff() ? 0.0f : m;     // (a row that has seen no key yet)
-      float sum = 0.0f;
 #pragma unroll
-      for (int x = 0; x < 8; ++x) { p[x] = att_exp2(p[x] - base); sum += p[x]; }
-      l += sum;
-      // the probabilities, at most 1, as the 16-bit operand of the second product: each is off by at most half a
-      // step of the type, which is what the output's own rounding is off by
+      for (int x = 0; x < 8; ++x) p[x] = att_exp2(p[x] - base) * LIFT;
+      // the probabilities, at most LIFT, as the 16-bit operand of the second product: each is off by at most half a
+      // step of the type (those of normal size, which reach down to 2^-29 of the largest in fp16), which is what the output's own
+      // rounding is off by; the sum is that of the rounded ones
       const u32x4_t pf = {pack2<DT>(p[0], p[1]), pack2<DT>(p[2], p[3]), pack2<DT>(p[4], p[5]), pack2<DT>(p[6], p[7])};
+      l = mfma16<DT>(ones, pf, l);
       if (!masked || !odd_v) {
 #pragma unroll
         for (int c = 0; c < NC; ++c)
@@ -434,9 +436,8 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
         if (d == 0) P.part_ml[which * ROWS + r] = make_float2(mm, ll);
       }
     };
-    const float lsum = quarters_sum(l);
     __syncthreads();                                            // (the buffer's last readers are done)
-    if (quarter == 0) { merge_ml[(wave * 16 + col) * 2] = m; merge_ml[(wave * 16 + col) * 2 + 1] = lsum; }
+    if (quarter == 0) { merge_ml[(wave * 16 + col) * 2] = m; merge_ml[(wave * 16 + col) * 2 + 1] = l[0]; }
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -491,8 +492,9 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
 //  - there is no maximum in the common case.  The reference m of a row is set so that the largest probability is 2^-REF; a
 //    later score may pass it, and only if a probability is then too large for the type's comfort (att_large) are
 //    the maximum, the rescaling of O and l and the probabilities formed (again, from the keys, which are still in LDS).
-//    Precision is relative in both types: bf16 takes REF = 16 and lets a probability grow to 2; fp16, whose smallest
-//    normal number is 2^-14, takes 0 and lets one grow to 2^15.
+//    A probability's precision is relative while it is a normal number: bf16 takes REF = 16 and lets a probability grow to 2, and
+//    has normal numbers down to 2^-126; fp16, whose smallest is 2^-14 (2^-25 and less is nothing), takes -12 and lets one grow until
+//    it is infinite, so that what lies less than 2^26 below a new maximum keeps all its bits.
 template <int DP> struct AttTile {
   static constexpr int STAGE = DP == 256 ? 32 : 64;
   static constexpr int THREADS = 512, RING = 4, IDS = 1024, LDS = RING * 2 * STAGE * DP * 2 + IDS * 4;
@@ -500,7 +502,7 @@ template <int DP> struct AttTile {
 __device__ const u32x4_t att_zeros = {0u, 0u, 0u, 0u};
 
 // Whether a probability needs a new reference: a running value over packed pairs, and its test.  bf16: one of 2 or more
-// has a bit of its own.  fp16: one of 2^15 or more, found behind the pairs' maximum.  Infinity and NaN count in both.
+// has a bit of its own.  fp16: one that is infinite (above 65504), found behind the pairs' maximum.  Infinity and NaN count in both.
 template <int DT> __device__ __forceinline__ uint32_t att_larger(uint32_t any, uint32_t lo, uint32_t hi) {
   if constexpr (DT == DT_F16) {
     typedef unsigned short pair_t __attribute__((ext_vector_type(2)));
@@ -508,7 +510,7 @@ template <int DT> __device__ __forceinline__ uint32_t att_larger(uint32_t any, u
   } else return any | lo | hi;
 }
 template <int DT> __device__ __forceinline__ bool att_large(uint32_t any) {
-  if constexpr (DT == DT_F16) return ((any | (any + 0x08000800u)) & 0x80008000u) != 0;
+  if constexpr (DT == DT_F16) return ((any | (any + 0x04000400u)) & 0x80008000u) != 0;
   else return (any & 0x40004000u) != 0;
 }
 
@@ -568,7 +570,7 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
   constexpr int RPI = 64 / CH, NL = WROWS / RPI; // rows of one load instruction, load instructions
   constexpr int HALVES = STAGE / 32;
   constexpr int BUF = STAGE * ROWB;              // bytes of K (of V) of a stage
-  constexpr float REF = DT == DT_F16 ? 0.0f : 16.0f, NONE = 1.0e30f;
+  constexpr float REF = DT == DT_F16 ? -12.0f : 16.0f, NONE = 1.0e30f;
   constexpr uint32_t ONES = DT == DT_F16 ? 0x3c003c00u : 0x3f803f80u;
   static_assert(NL * RPI == WROWS, "whole load instructions");
   extern __shared__ __attribute__((aligned(16))) unsigned char att_smem[];       // [RING][K, V][STAGE][ROWB], [IDS]
