@@ -428,7 +428,8 @@ int deinfer_rope_store(const void *q, int64_t ldq, int64_t n_q_heads,
  * row_start[s + 1] - 1) sees the cached[s] tokens before it and, of its sequence's rows, those in its bits of mask (as
  * deinfer_tree_mask makes them; any bits are taken as they are; rows without a bit in mask_words words are not
  * seen); mask = NULL: the rows up to its own.  A row that sees no key gives zeros.  Keys in blocks whose id is
- * outside [0, n_pool_blocks), and those beyond the table's row, are not seen.  What a row does not see has no
+ * outside [0, n_pool_blocks), and those beyond the table's row, are not seen.  Scores may have any size that fp32 has; a row whose
+ * scores are all minus infinity gives zeros too.  What a row does not see has no
  * influence, infinities and NaN included.  Padding rows of out are left as they are.
  *   q, out: T x (n_q_heads head_dim), pitches ldq, ldo; k_pool, v_pool: n_pool_blocks * block_tokens rows of n_kv_heads
  *   head_dim, pitches ldk, ldv; block_table: device int32 [n_seqs][table_pitch], at least ceil((cached + rows) /

@@ -570,7 +570,7 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
   constexpr int RPI = 64 / CH, NL = WROWS / RPI; // rows of one load instruction, load instructions
   constexpr int HALVES = STAGE / 32;
   constexpr int BUF = STAGE * ROWB;              // bytes of K (of V) of a stage
-  constexpr float REF = DT == DT_F16 ? -12.0f : 16.0f, NONE = 1.0e30f;
+  constexpr float REF = DT == DT_F16 ? -12.0f : 16.0f, NONE = 3.402823466e38f, FAR = 16777216.0f;
   constexpr uint32_t ONES = DT == DT_F16 ? 0x3c003c00u : 0x3f803f80u;
   static_assert(NL * RPI == WROWS, "whole load instructions");
   extern __shared__ __attribute__((aligned(16))) unsigned char att_smem[];       // [RING][K, V][STAGE][ROWB], [IDS]
@@ -611,7 +611,8 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
       }
     }
     f32x4_t o[RT][NF], l[RT];
-    float ref[RT];                               // -m; NONE where a row has seen no key yet: any score but minus infinity then makes an infinity
+    float ref[RT];                               // -m; NONE, fp32's largest number, where a row has seen no key yet: any score but minus infinity then makes an infinity
+    bool far_off = false;                        // some row's reference is FAR or more in size (see below)
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       ref[rt] = NONE; l[rt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -802,7 +803,7 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
         probabilities(sc, 1);
         __builtin_amdgcn_sched_barrier(0);
         scores(kf[1], sc, 1);
-        if (__any(att_large<DT>(any))) {
+        if (__any(att_large<DT>(any)) || far_off) {
           f32x4_t x[RT][2];
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
@@ -818,8 +819,13 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
             for (int u = 0; u < 2; ++u)
 #pragma unroll
               for (int i = 0; i < 4; ++i) top = fmaxf(top, x[rt][u][i]);
-            top = quarters_max(top) * P.scale2 + REF;
-            const float ref_new = top == -__builtin_inff() ? ref[rt] : fminf(ref[rt], -top);
+            top = quarters_max(top) * P.scale2;
+            // The fused product above has more bits than the rounded one that the reference is made of: beside a reference of 2^24 (FAR)
+            // the difference is a factor of up to 2, beside one of 2^31 an infinity or nothing.  From FAR on the wavefront rounds the
+            // products, takes the maximum of every 32 keys, and a row's largest probability is 1.
+            const bool seen = top != -__builtin_inff(), far = seen && fabsf(top) >= FAR;
+            far_off |= __any(far) != 0;
+            const float ref_new = !seen ? ref[rt] : fminf(ref[rt], far ? -top : -(top + REF));
             const float a = att_exp2(ref_new - ref[rt]);       // (0 from NONE on)
             ref[rt] = ref_new;
 #pragma unroll
@@ -829,8 +835,24 @@ __global__ __launch_bounds__(512, 2) void tree_attention_tile_kernel(const AttPa
 #pragma unroll
               for (int i = 0; i < 4; ++i) o[rt][f][i] *= a;
           }
+          if (far_off) {
 #pragma unroll
-          for (int u = 0; u < 2; ++u) probabilities(x, u);
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                float p[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  float t = x[rt][u][i] * P.scale2;
+                  asm volatile("" : "+v"(t));    // (not fused with the sum)
+                  p[i] = att_exp2(t + ref[rt]);
+                }
+                pf[rt][2 * u] = pack2<DT>(p[0], p[1]); pf[rt][2 * u + 1] = pack2<DT>(p[2], p[3]);
+              }
+          } else {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) probabilities(x, u);
+          }
         }
         if (!odd_v) {
           uint2 va[2][2];

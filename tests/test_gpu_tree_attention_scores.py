@@ -1,5 +1,6 @@
 """Attention over the paged cache where the scores are not those of an ordinary step: one key far above all others (whose
-weight may still be nearly all of the output, if that key's value is zero).  Against the formula in 64 bits.
+weight may still be nearly all of the output, if that key's value is zero), scores of any size that fp32 has.  Against the
+formula in 64 bits.
 
 Tolerance of a long tail, relative to the output itself (all values have one sign): the probabilities' rounding and the output's,
 half a step each, h = 2^-11 for fp16 and 2^-8 for bf16, and the numerator's and the sum's additions in fp32: one per 32 keys,
@@ -7,7 +8,7 @@ half a step each, h = 2^-11 for fp16 and 2^-8 for bf16, and the numerator's and 
 import numpy as np
 import pytest
 
-from test_gpu_cache_step import HALF, dn, ints, kind_of, wide  # noqa: F401
+from test_gpu_cache_step import HALF, cache_case, check_attention, dn, ints, kind_of, random_mask, wide  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +48,40 @@ def test_the_tail_below_one_key_that_has_no_value(dn, new, D, dtype, seqs, keys,
         ref = w[:n] @ vh[:n] / np.sum(w[:n])
         off = np.max(np.abs(got[:, i] - ref) / ref)
         assert off <= 2.02 * HALF[dtype] + 6e-4, (i, off)
+
+
+@pytest.mark.parametrize("words", [0, 2])
+@pytest.mark.parametrize("new,D", [([1, 1], 64), ([3, 2], 128), ([20, 9], 128), ([40, 33], 64), ([40, 33], 128), ([20, 30], 256)])
+@pytest.mark.parametrize("dtype,sizes", [("bf16", [1.0, 100.0, 1e6, 1e9, 1e12, 1e20, 1e30, 5e36]), ("f16", [1e-3, 0.1, 10.0, 1000.0, 60000.0])])
+def test_scores_of_any_size(dn, dtype, sizes, new, D, words):
+    """A row's scores are one factor of its own, up to 5e36 and of either sign, times a number of the key: from an ordinary
+    softmax to one key (or a few with the same number) that has all the weight.  The scores are exact in fp32, and where they are large
+    any two that differ are a weight of nothing apart, so the tolerance is that of ordinary ones."""
+    import torch
+    cached, hq, hk, bt = [700, 130], 4, 1, 16
+    table, k, v = cache_case(51, cached, new, hk, D, bt, dtype)
+    rng = np.random.default_rng(4)
+    start = np.concatenate([[0], np.cumsum(new)])
+    T = int(start[-1])
+    kk = torch.zeros((k.shape[0], D), dtype=torch.float64)
+    kk[:, 3] = torch.tensor(np.clip(rng.standard_normal(k.shape[0]), -4, 4) * (8000.0 if dtype == "f16" else 1.0))
+    k[:] = torch.where(torch.isnan(k), k, kk.to(k.dtype).cuda())
+    q = torch.zeros((T, hq, D), dtype=torch.float64)
+    q[:, :, 3] = torch.tensor(rng.choice(sizes, (T, hq)) * rng.choice([-1.0, 1.0], (T, hq)))
+    mask = random_mask(rng, new, words, T) if words else None
+    check_attention(dn, q.view(T, hq * D).to(k.dtype).cuda(), k, v, table, start, cached, hq, hk, bt, dtype, mask, scale=1.0)
+
+
+@pytest.mark.parametrize("new,D", [([1], 64), ([20], 128), ([40], 64), ([20], 256)])
+@pytest.mark.parametrize("dtype,q_value,k_value", [("bf16", 1e16, -1e16), ("bf16", 1e9, 2.0), ("bf16", 2.0 ** 62, -2.0 ** 63), ("f16", 60000.0, -30000.0), ("f16", 60000.0, 400.0)])
+def test_equal_scores_of_any_size(dn, dtype, q_value, k_value, new, D):
+    """Every score of a row is the same number, however large: every key that it sees has the same weight."""
+    import torch
+    cached, hq, hk, bt = [500], 4, 1, 16
+    table, k, v = cache_case(53, cached, new, hk, D, bt, dtype)
+    kk = torch.zeros_like(k)
+    kk[:, 0] = k_value
+    k[:] = torch.where(torch.isnan(k), k, kk)
+    q = torch.zeros((new[0], hq, D), dtype=k.dtype, device="cuda")
+    q[:, :, 0] = q_value
+    check_attention(dn, q.view(new[0], hq * D), k, v, table, np.array([0, new[0]]), cached, hq, hk, bt, dtype, scale=1.0)
