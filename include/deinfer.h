@@ -328,8 +328,8 @@ int deinfer_lowrank_up_rope(const void *t, int64_t T, int64_t ldt, const deinfer
  *                   in the table), and its position, cached + its index (padding: 0).
  *   counts:         device int32 [4], out: [0] new tokens in all (more than T: the rest has no rows and gets no
  *                   blocks), [1] blocks taken, [2] blocks that were needed and not to be had, [3] free_first + [1].
- * free_first must not point into counts (copy counts[3] to it between steps).  T = 0 writes nothing, row_start and counts
- * included.
+ * free_first must not point into counts (copy counts[3] to it between steps).  T = 0 takes no blocks; row_start and counts are
+ * written (unless both are NULL), slots and positions may be NULL.
  */
 #define DEINFER_KV_MAX_SEQS 8192
 int deinfer_kv_step(const int32_t *cached, const int32_t *n_new, int64_t n_seqs,

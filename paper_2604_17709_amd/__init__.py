@@ -582,7 +582,8 @@ class KvStep(NamedTuple):
 
 def deinfer_kv_step(cached, n_new, block_table, free_list, block_tokens: int, n_pool_blocks: int, rows: int, free_first=None,
                     out: Optional[KvStep] = None, stream=None) -> KvStep:
-    """Block tables (updated in place), slots and positions of a step's tokens from the requests' lengths."""
+    """Block tables (updated in place), slots and positions of a step's tokens from the requests' lengths.  With no rows,
+    row_start and counts are written as ever: no blocks are taken, counts[3] is free_first."""
     import torch
     n = cached.numel()
     _ints("cached", cached)

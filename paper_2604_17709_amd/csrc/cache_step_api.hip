@@ -109,8 +109,8 @@ int deinfer_kv_step(const int32_t *cached, const int32_t *n_new, int64_t n_seqs,
   if (int rc = check_pages("kv step", n_seqs, table_pitch, n_pool_blocks, block_tokens)) return rc;
   if (T < 0 || n_free < 0) return fail(DEINFER_ERR_INVALID_ARG, "kv step: negative size");
   if (T > MAX_ROWS || n_free > INT32_MAX / 2) return fail(DEINFER_ERR_UNSUPPORTED, "kv step: more than 2^28 rows or 2^30 free blocks");
-  if (T == 0) return DEINFER_OK;
-  if (!row_start || !slots || !positions || !counts) return fail(DEINFER_ERR_INVALID_ARG, "kv step: an output is NULL");
+  if (T == 0 && !row_start && !counts) return DEINFER_OK;
+  if (!row_start || !counts || (T > 0 && (!slots || !positions))) return fail(DEINFER_ERR_INVALID_ARG, "kv step: an output is NULL");
   if (n_seqs > 0 && (!cached || !n_new || (table_pitch > 0 && !block_table))) return fail(DEINFER_ERR_INVALID_ARG, "kv step: lengths or block table are NULL");
   if (n_free > 0 && !free_list) return fail(DEINFER_ERR_INVALID_ARG, "kv step: free_list is NULL");
   if (free_first && free_first >= counts && free_first < counts + 4) return fail(DEINFER_ERR_INVALID_ARG, "kv step: free_first must not lie in counts");
@@ -123,7 +123,7 @@ int deinfer_kv_step(const int32_t *cached, const int32_t *n_new, int64_t n_seqs,
   P.table_pitch = table_pitch; P.n_free = n_free; P.n_pool_blocks = n_pool_blocks;
   P.n_seqs = (int)n_seqs; P.block_tokens = (int)block_tokens; P.T = (int)T;
   P.vec = aligned(slots, 16) && aligned(positions, 16);
-  const int64_t groups = ceil_div(T, (int64_t)STEP_THREADS * STEP_ROWS);
+  const int64_t groups = T > 0 ? ceil_div(T, (int64_t)STEP_THREADS * STEP_ROWS) : 1;
   hipLaunchKernelGGL(kv_step_kernel, dim3((unsigned)(groups < 512 ? groups : 512)), dim3(STEP_THREADS), 0, static_cast<hipStream_t>(stream), P);
   return check_launch("kv step");
 }

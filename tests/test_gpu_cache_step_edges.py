@@ -1,0 +1,28 @@
+"""The calls of a step over the paged cache at the ends of their ranges."""
+import numpy as np
+import pytest
+
+from oracle import cache_step as cs
+from test_gpu_cache_step import dn, host, ints  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("first", [0, 3])
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("cached,new", [([], []), ([5, 0, 40], [0, 0, 0]), ([5, 0, 40], [2, 30, 1])])
+def test_a_step_without_rows(dn, cached, new, first, given):
+    """row_start and counts are written: a program may carry counts[3] on as the next step's free_first."""
+    import torch
+    bt, n_pool, free, n = 16, 20, list(range(10, 20)), len(cached)
+    table = np.arange(n * 4).reshape(n, 4) % 9
+    tab = ints(table)
+    z = lambda k: torch.full((k,), 77, dtype=torch.int32, device="cuda")
+    junk = [z(m) for m in (4096, 64, 16)]                            # (what the next allocations are likely to hold)
+    del junk
+    out = dn.KvStep(z(n + 1), z(0), z(0), z(4)) if given else None
+    got = dn.deinfer_kv_step(ints(cached), ints(new), tab, ints(free), bt, n_pool, 0, free_first=ints([first]) if first else None, out=out)
+    want = cs.kv_step(cached, new, table, free, first, n_pool, bt, 0)
+    assert host(got.row_start).tolist() == [0] * (n + 1) == want[0].tolist()
+    assert host(got.counts).tolist() == want[4].tolist() == [sum(new), 0, 0, first]
+    assert got.slots.numel() == 0 and got.positions.numel() == 0 and np.array_equal(host(tab), table)
