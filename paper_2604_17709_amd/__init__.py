@@ -673,7 +673,8 @@ def deinfer_rope_frequencies(rot_dim: int, theta: float = 10000.0, kind: int = R
 def deinfer_rope_store(q, k, v, positions, freqs, n_q_heads: int, n_kv_heads: int, head_dim: int, interleaved: bool = False,
                        magnitude: float = 1.0, slots=None, q_out=None, k_out=None, v_out=None, stream=None):
     """Queries rotated, keys rotated and values copied into their slots of the cache.  q, k and v may each be None; q_out, k_out
-    and v_out default to them (k and v: without slots only).  freqs: float64 device tensor [rot_dim / 2], or None to copy."""
+    and v_out default to them (k and v: without slots only).  freqs: float64 device tensor [rot_dim / 2], or None to copy.  A row
+    whose slot is negative or behind the pools' last row is left out; with queries alone, one whose slot is negative."""
     import torch
     first = q if q is not None else k if k is not None else v
     if first is None:
@@ -715,7 +716,7 @@ def deinfer_rope_store(q, k, v, positions, freqs, n_q_heads: int, n_kv_heads: in
     (qp, ldq, qo, ldqo), (kp, ldk, ko, ldko), (vp, ldv, vo, ldvo) = args
     _check(lib().deinfer_rope_store(qp, ldq, int(n_q_heads), kp, ldk, vp, ldv, int(n_kv_heads), rows, int(head_dim),
                                     0 if freqs is None else 2 * freqs.numel(), int(interleaved), _ptr(positions), _ptr(freqs), float(magnitude),
-                                    _ptr(slots), n_slots or 0, qo, ldqo, ko, ldko, vo, ldvo, _dtype_code(first), _stream(stream)))
+                                    _ptr(slots), 1 << 31 if n_slots is None else n_slots, qo, ldqo, ko, ldko, vo, ldvo, _dtype_code(first), _stream(stream)))
     return q_out, k_out, v_out
 
 

@@ -26,3 +26,20 @@ def test_a_step_without_rows(dn, cached, new, first, given):
     assert host(got.row_start).tolist() == [0] * (n + 1) == want[0].tolist()
     assert host(got.counts).tolist() == want[4].tolist() == [sum(new), 0, 0, first]
     assert got.slots.numel() == 0 and got.positions.numel() == 0 and np.array_equal(host(tab), table)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_queries_alone_with_slots(dn, in_place):
+    """Without a pool beside them every slot that is not negative is one in use; a row without one is left as it is."""
+    import torch
+    rows, heads, D = 5, 2, 32
+    q = torch.randn(rows, heads * D, device="cuda").bfloat16()
+    f = torch.tensor(cs.frequencies(D, 10000.0)[0], device="cuda")
+    pos, slots = ints([3, 1000, 7, 0, 99]), ints([4, 0, -1, 2 ** 31 - 1, 123456])
+    want = q.clone()
+    dn.deinfer_rope_store(want, None, None, pos, f, heads, 0, D)
+    mine, out = q.clone(), torch.full_like(q, 3.0)
+    got, k_out, v_out = dn.deinfer_rope_store(mine, None, None, pos, f, heads, 0, D, slots=slots, q_out=None if in_place else out)
+    assert got is (mine if in_place else out) and k_out is None and v_out is None
+    used = torch.tensor([0, 1, 3, 4], device="cuda")
+    assert torch.equal(got[used], want[used]) and torch.equal(got[2], q[2] if in_place else torch.full_like(q[2], 3.0))
