@@ -226,13 +226,14 @@ int deinfer_rope_store(const void *q, int64_t ldq, int64_t n_q_heads, const void
   if (T > MAX_ROWS || head_dim > MAX_PITCH || n_q_heads > MAX_PITCH / head_dim || n_kv_heads > MAX_PITCH / head_dim)
     return fail(DEINFER_ERR_UNSUPPORTED, "rope store: sizes out of range");
   const bool have_q = n_q_heads > 0 && q, have_k = n_kv_heads > 0 && k, have_v = n_kv_heads > 0 && v;
+  if (T == 0) return DEINFER_OK;                 // (rows that are none have no address either)
   if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr) || (v == nullptr) != (v_out == nullptr))
     return fail(DEINFER_ERR_INVALID_ARG, "rope store: q, k, v go together with q_out, k_out, v_out");
   if ((q && n_q_heads == 0) || ((k || v) && n_kv_heads == 0)) return fail(DEINFER_ERR_INVALID_ARG, "rope store: no heads");
   const int64_t wq = n_q_heads * head_dim, wk = n_kv_heads * head_dim;
   if ((have_q && (ldq < wq || ldqo < wq)) || (have_k && (ldk < wk || ldko < wk)) || (have_v && (ldv < wk || ldvo < wk)))
     return fail(DEINFER_ERR_INVALID_ARG, "rope store: a pitch is smaller than heads * head_dim");
-  if (T == 0 || !(have_q || have_k || have_v)) return DEINFER_OK;
+  if (!(have_q || have_k || have_v)) return DEINFER_OK;
   if (rot_dim > 0 && (have_q || have_k) && (!positions || !freqs)) return fail(DEINFER_ERR_INVALID_ARG, "rope store: positions or freqs is NULL");
   if (slots && ((have_k && k == k_out) || (have_v && v == v_out))) return fail(DEINFER_ERR_INVALID_ARG, "rope store: keys and values that go to slots cannot stay in place");
   if ((have_q && q == q_out && ldq != ldqo) || (have_k && k == k_out && ldk != ldko) || (have_v && v == v_out && ldv != ldvo))

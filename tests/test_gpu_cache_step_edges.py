@@ -43,3 +43,22 @@ def test_queries_alone_with_slots(dn, in_place):
     assert got is (mine if in_place else out) and k_out is None and v_out is None
     used = torch.tensor([0, 1, 3, 4], device="cuda")
     assert torch.equal(got[used], want[used]) and torch.equal(got[2], q[2] if in_place else torch.full_like(q[2], 3.0))
+
+
+def test_the_calls_of_a_step_without_rows(dn):
+    """Every call of a step takes a step without rows; the cache stays as it is."""
+    import torch
+    bt, n_pool, hq, hk, D = 16, 8, 4, 2, 64
+    cached, new, table = ints([5, 20]), ints([0, 0]), ints([[0, 1, 2], [3, 4, 5]])
+    step = dn.deinfer_kv_step(cached, new, table, ints([6, 7]), bt, n_pool, 0)
+    pools = [torch.full((n_pool * bt, hk * D), 3.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    qkv = torch.zeros((0, (hq + 2 * hk) * D), dtype=torch.bfloat16, device="cuda")
+    q, k, v = qkv[:, :hq * D], qkv[:, hq * D:(hq + hk) * D], qkv[:, (hq + hk) * D:]
+    f = torch.tensor(cs.frequencies(D, 10000.0)[0], device="cuda")
+    mask = torch.zeros((0, 1), dtype=torch.int32, device="cuda")
+    dn.deinfer_tree_mask(step.slots, step.row_start, cached, mask, step.positions)
+    dn.deinfer_rope_store(q, k, v, step.positions, f, hq, hk, D, slots=step.slots, k_out=pools[0], v_out=pools[1])
+    dn.deinfer_rope_store(q, k, v, step.positions, f, hq, hk, D, slots=step.slots, q_out=torch.zeros((4, hq * D), dtype=torch.bfloat16, device="cuda"), k_out=pools[0], v_out=pools[1])
+    ws = dn.Workspace(dn.deinfer_tree_attention_workspace_bytes(0, 2, hq, hk, D))
+    out = dn.deinfer_tree_attention(q, pools[0], pools[1], table, step.row_start, cached, ws, hq, hk, bt, mask=mask)
+    assert out.shape == (0, hq * D) and all(bool((p == 3.0).all()) for p in pools)
