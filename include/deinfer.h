@@ -400,7 +400,7 @@ int deinfer_tree_mask(const int32_t *parents, const int32_t *row_start, const in
  *   positions      device int32 [T]; freqs: device double [rot_dim / 2].  rot_dim = 0 only copies (rows of the low-rank cache).
  * dtype: of q, k, v and the outputs.  Any pitches and alignments; 16-byte aligned rows, head_dim and rot_dim / 2 (rot_dim
  * where interleaved) of whole 16-byte pieces take 16-byte loads and stores.  Angles in double precision, products in
- * fp32, one rounding.
+ * fp32, one rounding.  T <= 2^28.
  */
 enum { DEINFER_ROPE_PLAIN = 0, DEINFER_ROPE_LINEAR = 1, DEINFER_ROPE_BASE = 2, DEINFER_ROPE_BANDS = 3, DEINFER_ROPE_RAMP = 4 };
 typedef struct deinfer_rope_scaling {

@@ -91,7 +91,7 @@ int launch_attention_of(const AttPlan &pl, const AttParams &P, hipStream_t s) {
 
 template <typename TE>
 void launch_rope_store(const RopeStoreParams &P, bool vec, bool inter, hipStream_t s) {
-  const dim3 grid((unsigned)P.T), block(ROPE_THREADS);
+  const dim3 grid((unsigned)(P.T < ROPE_GRID ? P.T : ROPE_GRID), (unsigned)ceil_div(P.T, (int64_t)ROPE_GRID)), block(ROPE_THREADS);
   if (vec && inter) hipLaunchKernelGGL((rope_store_kernel<TE, 16 / sizeof(TE), true>), grid, block, 0, s, P);
   else if (vec) hipLaunchKernelGGL((rope_store_kernel<TE, 16 / sizeof(TE), false>), grid, block, 0, s, P);
   else if (inter) hipLaunchKernelGGL((rope_store_kernel<TE, 2, true>), grid, block, 0, s, P);

@@ -17,6 +17,7 @@ namespace deinfer {
 
 constexpr int ROPE_THREADS = 256;
 constexpr int ROPE_MAX_PAIRS = 512;
+constexpr int ROPE_GRID = 1 << 20;               // tokens of one row of the grid: its threads have to stay below 2^32
 
 struct RopeStoreParams {
   const void *q, *k, *v;
@@ -82,7 +83,8 @@ template <typename TE, int VE> struct Piece {
 template <typename TE, int VE, bool INTER>
 __global__ __launch_bounds__(ROPE_THREADS) void rope_store_kernel(const RopeStoreParams P) {
   __shared__ float cs[ROPE_MAX_PAIRS], sn[ROPE_MAX_PAIRS];
-  const int t = blockIdx.x, tid = threadIdx.x;
+  const int t = (int)blockIdx.y * ROPE_GRID + (int)blockIdx.x, tid = threadIdx.x;
+  if (t >= P.T) return;
   long long to = t;
   if (P.slots) {
     to = P.slots[t];

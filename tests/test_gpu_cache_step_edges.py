@@ -62,3 +62,23 @@ def test_the_calls_of_a_step_without_rows(dn):
     ws = dn.Workspace(dn.deinfer_tree_attention_workspace_bytes(0, 2, hq, hk, D))
     out = dn.deinfer_tree_attention(q, pools[0], pools[1], table, step.row_start, cached, ws, hq, hk, bt, mask=mask)
     assert out.shape == (0, hq * D) and all(bool((p == 3.0).all()) for p in pools)
+
+
+def test_rotary_store_of_more_rows_than_a_grid_has_threads_for(dn):
+    """2^24 + 3 rows, a workgroup each: more threads than 32 bits count.  Against the same call on a few of the rows."""
+    import torch
+    rows, D = (1 << 24) + 3, 2
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v = (torch.randn(rows, D, device="cuda", generator=g).bfloat16() for _ in range(3))
+    pos = torch.arange(rows, device="cuda", dtype=torch.int32)
+    slots = (rows - 1 - pos).contiguous()
+    f = torch.tensor([0.37], dtype=torch.float64, device="cuda")
+    pools = [torch.full((rows, D), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    some = torch.cat([torch.tensor([0, 1, (1 << 20) - 1, 1 << 20, (1 << 24) - 1, 1 << 24, rows - 1], device="cuda"), torch.randint(0, rows, (3000,), device="cuda", generator=g)])
+    want = [t[some].contiguous() for t in (q, k)]
+    dn.deinfer_rope_store(want[0], want[1], None, pos[some].contiguous(), f, 1, 1, D)
+    out = torch.full_like(q, 9.0)
+    dn.deinfer_rope_store(q, k, v, pos, f, 1, 1, D, slots=slots, q_out=out, k_out=pools[0], v_out=pools[1])
+    assert torch.equal(out[some], want[0]) and torch.equal(pools[0][slots[some].long()], want[1])
+    assert torch.equal(pools[1].flip(0), v)
+    assert bool((out != 9.0).all()) and bool((pools[0] != 9.0).all())
