@@ -366,8 +366,9 @@ int deinfer_kv_compact_plan_device(const int32_t *block_table, int64_t n_seqs, i
  *   row_start, cached: as of deinfer_kv_step.
  *   mask:      device uint32 [T][mask_words], out: bit j of a row (bit j % 32 of word j / 32) is set if the row's token
  *              sees token j of its sequence's rows: its ancestors and itself.  mask_words <= DEINFER_TREE_MAX_WORDS;
- *              rows beyond the 32 mask_words-th of a sequence get no bits.
- *   positions: device int32 [T], out, may be NULL: cached + number of ancestors.
+ *              rows beyond the 32 mask_words-th of a sequence get no bits: they see none of the step's tokens, themselves included.
+ *   positions: device int32 [T], out, may be NULL: cached + number of ancestors among its bits, i.e. cached for a row without
+ *              bits (mask_words has to cover the longest sequence's rows for its depths to be whole).
  * Padding rows are left as they are.
  */
 #define DEINFER_TREE_MAX_WORDS 32

@@ -639,7 +639,8 @@ def deinfer_kv_compact_plan_device(block_table, n_tokens, n_pool_blocks: int, bu
 
 
 def deinfer_tree_mask(parents, row_start, cached, mask, positions=None, stream=None):
-    """Visibility bits (int32 [rows, words], bit patterns) and positions of drafted trees from their tokens' parents."""
+    """Visibility bits (int32 [rows, words], bit patterns) and positions of drafted trees from their tokens' parents.  Rows of a
+    sequence from the 32 words-th on get no bits and the position of a token without ancestors."""
     n, rows = cached.numel(), parents.numel()
     _ints("parents", parents)
     _ints("cached", cached)

@@ -82,3 +82,19 @@ def test_rotary_store_of_more_rows_than_a_grid_has_threads_for(dn):
     assert torch.equal(out[some], want[0]) and torch.equal(pools[0][slots[some].long()], want[1])
     assert torch.equal(pools[1].flip(0), v)
     assert bool((out != 9.0).all()) and bool((pools[0] != 9.0).all())
+
+
+def test_rows_of_a_tree_behind_its_mask(dn):
+    """A chain of 70 tokens with one word of bits: rows 32 .. 69 see nothing drafted and count as tokens without ancestors; the row
+    before is whole, and so is every row with three words."""
+    import torch
+    n, c = 70, 11
+    parents, start, cached = ints(np.arange(n) - 1), ints([0, n]), ints([c])
+    for words in (1, 3):
+        mask, pos = torch.full((n, words), 5, dtype=torch.int32, device="cuda"), torch.full((n,), 5, dtype=torch.int32, device="cuda")
+        dn.deinfer_tree_mask(parents, start, cached, mask, pos)
+        j = np.arange(n)
+        inside = j < 32 * words
+        assert np.array_equal(host(pos), np.where(inside, c + j, c))
+        bits = (host(mask).view(np.uint32)[:, :, None] >> np.arange(32, dtype=np.uint32)) & 1
+        assert np.array_equal(bits.reshape(n, -1), np.tril(np.ones((n, 32 * words))) * inside[:, None])
