@@ -730,7 +730,8 @@ def deinfer_tree_attention_workspace_bytes(rows: int, n_seqs: int, n_q_heads: in
 def deinfer_tree_attention(q, k_pool, v_pool, block_table, row_start, cached, ws: Workspace, n_q_heads: int, n_kv_heads: int, block_tokens: int,
                            scale: Optional[float] = None, mask=None, out=None, stream=None):
     """Attention of a step's rows over the paged cache: k_pool, v_pool [slots, n_kv_heads * head_dim]; mask: int32 [rows, words]
-    visibility bits among a sequence's own rows (None: causal).  Rows behind the last sequence's keep what ``out`` holds."""
+    visibility bits among a sequence's own rows (None: causal).  Rows behind the last sequence's keep what ``out`` holds (a new
+    one: whatever its memory held)."""
     (rows, cols, ldq), n = _matrix(q, "q"), cached.numel()
     if n_q_heads <= 0 or cols % n_q_heads:
         raise ValueError("q: [rows, n_q_heads * head_dim] expected")
@@ -757,7 +758,7 @@ def deinfer_tree_attention(q, k_pool, v_pool, block_table, row_start, cached, ws
             raise ValueError("out: [rows, n_q_heads * head_dim] of q's dtype expected")
     _on_device(q, k_pool, v_pool, block_table, row_start, cached, mask, out, ws.buf)
     _check(lib().deinfer_tree_attention(_ptr(q), rows, ldq, int(n_q_heads), int(n_kv_heads), head_dim, _ptr(row_start), _ptr(cached), n,
-                                        _ptr(mask), words, _ptr(k_pool), ldk, _ptr(v_pool), ldv, n_slots // int(block_tokens),
-                                        int(block_tokens), _ptr(block_table), pitch, head_dim ** -0.5 if scale is None else float(scale),
+                                        _ptr(mask), words, _ptr(k_pool), ldk, _ptr(v_pool), ldv, n_slots // int(block_tokens) if block_tokens > 0 else 0,
+                                        int(block_tokens), _ptr(block_table), pitch, (head_dim or 1) ** -0.5 if scale is None else float(scale),
                                         _ptr(out), ldo, _dtype_code(q), _ptr(ws.buf), ws.nbytes, _stream(stream)))
     return out

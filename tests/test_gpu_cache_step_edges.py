@@ -98,3 +98,17 @@ def test_rows_of_a_tree_behind_its_mask(dn):
         assert np.array_equal(host(pos), np.where(inside, c + j, c))
         bits = (host(mask).view(np.uint32)[:, :, None] >> np.arange(32, dtype=np.uint32)) & 1
         assert np.array_equal(bits.reshape(n, -1), np.tril(np.ones((n, 32 * words))) * inside[:, None])
+
+
+def test_attention_refuses_blocks_of_no_tokens_and_heads_of_no_features(dn):
+    """As an error of the library, like every other size, and before a launch."""
+    import torch
+    x = torch.zeros((2, 64), dtype=torch.bfloat16, device="cuda")
+    ws = dn.Workspace(dn.deinfer_tree_attention_workspace_bytes(2, 1, 1, 1, 64))
+    for bt in (0, -16):
+        with pytest.raises(dn.DeinferError) as e:
+            dn.deinfer_tree_attention(x, x, x, ints([[0]]), ints([0, 2]), ints([0]), ws, 1, 1, bt)
+        assert e.value.code == dn.ERR_INVALID_ARG
+    with pytest.raises(dn.DeinferError) as e:
+        dn.deinfer_tree_attention(x[:, :0], x, x, ints([[0]]), ints([0, 2]), ints([0]), ws, 1, 1, 2)
+    assert e.value.code == dn.ERR_UNSUPPORTED
