@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from oracle import cache_step as cs
-from test_gpu_cache_step import dn, host, ints  # noqa: F401
+from test_gpu_cache_step import cache_case, check_attention, dn, host, ints, normal, random_mask  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -112,3 +112,19 @@ def test_attention_refuses_blocks_of_no_tokens_and_heads_of_no_features(dn):
     with pytest.raises(dn.DeinferError) as e:
         dn.deinfer_tree_attention(x[:, :0], x, x, ints([[0]]), ints([0, 2]), ints([0]), ws, 1, 1, 2)
     assert e.value.code == dn.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("spare", [0, 1500])
+@pytest.mark.parametrize("dtype,hq,hk,D,words", [("bf16", 2, 2, 64, 0), ("f16", 8, 1, 128, 0), ("bf16", 4, 1, 128, 10)])
+def test_attention_of_a_batch_that_mixes_chunks_and_single_tokens(dn, dtype, hq, hk, D, words, spare):
+    """Forty single tokens and a chunk of 300: the rows of a tile go by the average, 16 here, and 128 or 256 where the buffer has
+    1500 rows to spare.  The result is the same."""
+    import torch
+    rng = np.random.default_rng(D)
+    cached, new = rng.integers(0, 200, 42), np.ones(42, dtype=int)
+    new[7], new[20] = 300, 0
+    table, k, v = cache_case(61, cached, new, hk, D, 16, dtype)
+    start = np.concatenate([[0], np.cumsum(new)])
+    T = int(start[-1]) + spare
+    q = torch.tensor(normal(62, T, hq * D), device="cuda").to(k.dtype)
+    check_attention(dn, q, k, v, table, start, cached, hq, hk, 16, dtype, random_mask(rng, new, words, T) if words else None)
