@@ -50,7 +50,9 @@ AttPlan att_plan(int64_t T, int64_t n_seqs, int64_t n_q, int64_t n_kv, int64_t h
   // Rows of a tile, by the rows there are.  Keys straight into registers for up to 16 rows (8 x 1000 cached tokens, 8 key heads
   // of 128: 18.4 us against 21.1 with tiles of 128; 8 x 4000: 37.5 and 37.3; with 24 rows 54 and 37.6), tiles of 128 up to as many
   // (8 x 4000 with 128 rows: 52 against 54 with 256; 32 x 4000: 122 and 120; 160 rows: 224 and 157).  The sums of 256 rows of 256
-  // features have no room in the registers.
+  // features have no room in the registers.  One choice for all sequences, from the rows that the buffer has: 255 single tokens
+  // on up to 4000 and a chunk of 2048 on 2000 take 588 us in 16-row tiles where the two parts alone take 433 + 77 (8 query and
+  // key heads of 128; with 64 query heads 827 and 442 + 284), the single tokens in a buffer with 8192 rows 420 (467 against 442).
   p.rows = per_head <= 16 ? 16 : p.dp == 256 || per_head <= 128 ? 128 : 256;
   const int cus = device_cus();
   p.shares = (p.rows == 16 ? 2 : 1) * (int64_t)(cus > 0 ? cus : 256);

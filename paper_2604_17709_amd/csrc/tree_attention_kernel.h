@@ -473,17 +473,20 @@ __global__ __launch_bounds__(ATT_THREADS) void tree_attention_kernel(const AttPa
 // The same work where a sequence and key head has more than a few rows: eight wavefronts with RT tiles of 16 rows each
 // share the keys, STAGE at a time, through LDS, a ring of four stages.  The rows of K and V come straight from
 // memory into the ring, three stages ahead of their use (no registers, no waiting; one barrier per stage).  Rows
-// lie in LDS as they do in memory but for their 16-byte pieces, which are XORed with the row's number: sixteen rows at one
-// place (an operand of K), and four neighbouring features of sixteen rows (the transposing read that makes V^T's
-// operand), then cover all banks.  V needs no permutes here, and its features keep their order: block f of the
-// output is 16 f .. 16 f + 15.
+// lie in LDS as they do in memory but for their 16-byte pieces, which are XORed with the row's number.  With heads of 128 and 256
+// sixteen rows at one place (an operand of K) then cover all banks; with heads of 64, whose rows are half of the banks
+// wide, rows r and r + 8 meet.  The transposing read that makes V^T's operand takes the pieces 2 f and 2 f + 1 of its rows, and the
+// XOR only swaps those two between the rows 2 n and 2 n + 1: with heads of 128 it covers half of the banks twice, two cycles of conflict
+// per read (SQ_LDS_BANK_CONFLICT: 1.45e7 cycles in 7.3e6 such reads).  V needs no permutes here, and its features keep their
+// order: block f of the output is 16 f .. 16 f + 15.
 //
 // Measured (64 drafted tokens x 16 sequences of up to 16384 keys, 8 key heads of 128, fp16): 339 us a call, about 4200 cycles for
-// 64 keys and 256 rows, of which 2176 are matrix instructions (two wavefronts per SIMD) and 2048 the LDS reads of
-// all eight wavefronts at the full rate; 2 x 2048 prompt tokens on up to 6000 cached, 32 heads, bf16: 417 us = 829 TFLOP/s.
+// 64 keys and 256 rows.  2176 of them are matrix instructions (two wavefronts per SIMD); the LDS reads of all eight wavefronts
+// are 256 KiB, 2048 cycles at 128 bytes each, and 512 cycles of conflicts.  2 x 2048 prompt tokens on up to 6000 cached, 32 heads,
+// bf16: 411 us = 816 TFLOP/s.
 // Under such calls the clock falls to its power limit (half of the wavefronts asleep for 640 cycles of every stage cost nothing), so
 // fewer instructions count for more than a better overlap: one look at a table's entry per wavefront where all keys of a stage
-// exist, instead of one per lane, 433 -> 419, the reference kept as it is used, 411 to 416.  Four wavefronts of 64 rows read half as much from LDS, but one
+// exist, instead of one per lane, took the prompts' call from 433 to 419 us, the reference kept as it is used to 411 to 416.  Four wavefronts of 64 rows read half as much from LDS, but one
 // wavefront per SIMD has nothing to run beside its own vector instructions: 5500 cycles.
 //
 // The scores of the 32 keys after are multiplied while those of these are turned into probabilities, and
