@@ -85,3 +85,30 @@ def test_equal_scores_of_any_size(dn, dtype, q_value, k_value, new, D):
     q = torch.zeros((new[0], hq, D), dtype=k.dtype, device="cuda")
     q[:, :, 0] = q_value
     check_attention(dn, q.view(new[0], hq * D), k, v, table, np.array([0, new[0]]), cached, hq, hk, bt, dtype, scale=1.0)
+
+
+@pytest.mark.parametrize("D,new,hq", [(64, 4, 2), (128, 4, 4), (128, 20, 4), (64, 50, 4), (256, 40, 4)])
+@pytest.mark.parametrize("value", [float("inf"), -float("inf"), float("nan")])
+def test_fp16_values_that_are_no_numbers(dn, D, new, hq, value):
+    """A drafted token's value is no number: rows whose mask leaves it out stay within the tolerance of finite values of the formula
+    (those of ``check_attention``), the others have it in that feature alone."""
+    cached, bt, bad = [90], 16, 1
+    table, k, v = cache_case(55, cached, [new], 1, D, bt, "f16")
+    rng = np.random.default_rng(7)
+    mask = random_mask(rng, [new], 2, new)
+    mask[0, 0] &= ~np.uint32(1 << bad)
+    mask[new - 1, 0] |= np.uint32(1 << bad)
+    import torch
+    q = torch.tensor(rng.standard_normal((new, hq * D)), device="cuda").half()
+    want = check_attention(dn, q, k, v, table, np.array([0, new]), cached, hq, 1, bt, "f16", mask).reshape(new, hq, D)
+    slot = int(table[0, (cached[0] + bad) // bt]) * bt + (cached[0] + bad) % bt
+    v[slot, 3] = value
+    ws = dn.Workspace(dn.deinfer_tree_attention_workspace_bytes(new, 1, hq, 1, D))
+    got = wide(dn.deinfer_tree_attention(q, k, v, ints(table), ints([0, new]), ints(cached), ws, hq, 1, bt, mask=ints(mask.view(np.int32)))).reshape(new, hq, D)
+    sees = (mask[:, 0] >> np.uint32(bad)) & 1 != 0
+    assert sees.any() and not sees.all()
+    # (beside such a value the sums are formed one key at a time: fp32 sums in another order, 123 keys 2^-24, and a step of the output)
+    close = lambda a, b: np.all(np.abs(a - b) <= 2 * HALF["f16"] * np.abs(b) + 2e-5 * np.max(np.abs(want)) + 2.0 ** -24)
+    assert close(got[~sees], want[~sees])
+    assert close(np.delete(got[sees], 3, axis=2), np.delete(want[sees], 3, axis=2))
+    assert np.all(np.isnan(got[sees][:, :, 3]) if value != value else got[sees][:, :, 3] == value)
