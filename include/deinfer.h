@@ -455,6 +455,74 @@ int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_he
                            void *out, int64_t ldo, int dtype, void *ws, size_t ws_bytes, void *stream);
 
 /*
+ * Between the projections of a prompt: positions of several axes, norms of queries and keys with their rotation, and
+ * attention over the rows of keys and values as the projections write them, with no pages between.  Lengths and positions are in device
+ * memory, so that one captured graph serves every step; rows behind the last sequence's are padding and left as they are.
+ *
+ * deinfer_axis_positions: positions (time, height, width) of a step's tokens, for requests that mix text with images and video.
+ *   segments:       device int32 [n_segments][4], 16-byte aligned: {t, h, w, step}.  h or w not positive: text of t tokens; else a
+ *                   grid of t x h x w tokens, frame by frame and row by row.  t not positive: no tokens; a negative step is 0.
+ *   segment_start:  device int32 [n_seqs + 1]: first segment of every request, and the end of the last.
+ *   row_start, cached: as of deinfer_kv_step; cached NULL: zeros.  Row i of a sequence is token cached + i of its request;
+ *                   tokens behind the last segment are text.
+ *   positions:      device int32 [3][pitch], out.  A segment that begins at p: text token i stands at p + i on every axis, grid token
+ *                   (a, b, c) at (p + step a, p + b, p + c); the next segment begins at the largest of these + 1.  Positions end
+ *                   at 2^31 - 1.
+ * At most DEINFER_KV_MAX_SEQS sequences; T, n_segments <= 2^28.
+ *
+ * deinfer_rope_axes (host only): the axis of every rotated pair, axis_of[i], i < rot_dim / 2, from the number of pairs of each of
+ * 1 .. DEINFER_ROPE_MAX_AXES axes (rot_dim / 2 in all): axis after axis, or, if turns is not 0, given out by turns, an axis
+ * dropping out when it has its pairs.
+ *
+ * deinfer_norm_rope_store: deinfer_rope_store with a norm of every head of the queries and keys ahead of the rotation, and
+ * positions of several axes.
+ *   q_weight, k_weight: device [head_dim], of dtype; each may be NULL: that side is not normed.  A normed head is
+ *                   w x / sqrt(mean x^2 + eps), its elements from rot_dim on too; values are copied.
+ *   positions:      device int32 [n_axes][pos_pitch]; pair i is rotated by positions[axis_of[i]][t] freqs[i].  axis_of: device uint8
+ *                   [rot_dim / 2] (may be NULL with one axis; an axis that there is not counts as 0).
+ * Everything else as of deinfer_rope_store: pitches, slots, outputs in place.  Sums and products in fp32 (a sum out of fp32's
+ * range in 64 bits), angles in double precision, one rounding.  head_dim <= DEINFER_NORM_MAX_DIM, T <= 2^28.
+ *
+ * deinfer_prompt_attention: attention of packed sequences: prompts, chunks behind others' keys, images whose patches all see
+ * each other, single tokens over rebuilt keys and values.
+ *   out[t, h] = sum_j p_j v_j, p = softmax over the keys j that row t sees of scale (q[t, h] . k_j)
+ * where query head h reads key head h / (n_q_heads / n_kv_heads).
+ *   q_start, k_start: device int32 [n_seqs + 1]: first row of every sequence in q and out, in k and v, and the end of the last; k_start
+ *                   NULL: q_start.  Row i of a sequence with n rows and m keys stands at p = m - n + i (the last row at the last key)
+ *                   and sees its keys j, p - left <= j <= p + right; a negative side has no bound (causal: left = -1, right = 0).  A row that sees
+ *                   no key gives zeros; so does one whose scores are all minus infinity.  What a row does not see has no
+ *                   influence, infinities and NaN included.
+ *   q, out: T x (n_q_heads head_dim), pitches ldq, ldo; k, v: n_keys x (n_kv_heads head_dim), pitches ldk, ldv.  16-byte aligned,
+ *                   pitches multiples of 8.  out must not overlap the others.
+ *   dtype: bf16 or fp16.  head_dim: a multiple of 8, at most 256.  scale: a normal positive number of fp32, with 1 / ln 2 on it too.
+ * Arithmetic as of deinfer_tree_attention: fp32 throughout, probabilities rounded to the storage type for the second product, their
+ * sum that of the rounded ones, one rounding of the output.  Results do not depend on timing.  The workspace
+ * (deinfer_prompt_attention_workspace_bytes, host only; 256-byte aligned) needs no clearing and serves one call at a time; its size is that of
+ * the call's own T and n_seqs.  T, n_keys <= 2^28, at most DEINFER_KV_MAX_SEQS sequences.
+ */
+#define DEINFER_ROPE_MAX_AXES 4
+#define DEINFER_NORM_MAX_DIM 2048
+int deinfer_axis_positions(const int32_t *segments, int64_t n_segments, const int32_t *segment_start,
+                           const int32_t *row_start, const int32_t *cached, int64_t n_seqs, int64_t T,
+                           int32_t *positions, int64_t pitch, void *stream);
+int deinfer_rope_axes(int64_t rot_dim, int64_t n_axes, const int32_t *pairs, int turns, uint8_t *axis_of);
+int deinfer_norm_rope_store(const void *q, int64_t ldq, int64_t n_q_heads,
+                            const void *k, int64_t ldk, const void *v, int64_t ldv, int64_t n_kv_heads,
+                            int64_t T, int64_t head_dim, int64_t rot_dim, int interleaved,
+                            const void *q_weight, const void *k_weight, double eps,
+                            const int32_t *positions, int64_t pos_pitch, int64_t n_axes, const uint8_t *axis_of,
+                            const double *freqs, double magnitude, const int32_t *slots, int64_t n_slots,
+                            void *q_out, int64_t ldqo, void *k_out, int64_t ldko, void *v_out, int64_t ldvo,
+                            int dtype, void *stream);
+int deinfer_prompt_attention_workspace_bytes(int64_t T, int64_t n_seqs, int64_t n_q_heads, int64_t n_kv_heads,
+                                             int64_t head_dim, size_t *bytes);
+int deinfer_prompt_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads,
+                             int64_t head_dim, const int32_t *q_start,
+                             const void *k, int64_t ldk, const void *v, int64_t ldv, int64_t n_keys,
+                             const int32_t *k_start, int64_t n_seqs, int64_t left, int64_t right, double scale,
+                             void *out, int64_t ldo, int dtype, void *ws, size_t ws_bytes, void *stream);
+
+/*
  * MLP second sub-layer (Sec. 4.1): y = (h U_d) V_d with d_in = FFN width.
  * Same contract as deinfer_lowrank_linear.
  */

@@ -73,6 +73,8 @@ EXPORTS = [
     "deinfer_rope_table", "deinfer_lowrank_up_rope",
     "deinfer_kv_step", "deinfer_kv_compact_plan_device", "deinfer_tree_mask", "deinfer_rope_frequencies", "deinfer_rope_store",
     "deinfer_tree_attention_workspace_bytes", "deinfer_tree_attention",
+    "deinfer_axis_positions", "deinfer_rope_axes", "deinfer_norm_rope_store",
+    "deinfer_prompt_attention_workspace_bytes", "deinfer_prompt_attention",
 ]
 
 _lib = None
@@ -136,6 +138,13 @@ def lib() -> ctypes.CDLL:
         L.deinfer_tree_attention_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64, _i64, ctypes.POINTER(_sz)]
         L.deinfer_tree_attention.argtypes = [_vp, _i64, _i64, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64,
                                              _vp, _i64, ctypes.c_double, _vp, _i64, ctypes.c_int, _vp, _sz, _vp]
+        L.deinfer_axis_positions.argtypes = [_vp, _i64, _vp, _vp, _vp, _i64, _i64, _vp, _i64, _vp]
+        L.deinfer_rope_axes.argtypes = [_i64, _i64, _ip, ctypes.c_int, ctypes.POINTER(ctypes.c_uint8)]
+        L.deinfer_norm_rope_store.argtypes = [_vp, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _i64, _i64, ctypes.c_int, _vp, _vp, ctypes.c_double,
+                                              _vp, _i64, _i64, _vp, _vp, ctypes.c_double, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, ctypes.c_int, _vp]
+        L.deinfer_prompt_attention_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64, _i64, ctypes.POINTER(_sz)]
+        L.deinfer_prompt_attention.argtypes = [_vp, _i64, _i64, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _i64,
+                                               ctypes.c_double, _vp, _i64, ctypes.c_int, _vp, _sz, _vp]
         for name in EXPORTS:
             if name not in ("deinfer_last_error",):
                 getattr(L, name).restype = ctypes.c_int
@@ -671,15 +680,9 @@ def deinfer_rope_frequencies(rot_dim: int, theta: float = 10000.0, kind: int = R
     return freqs, float(magnitude.value)
 
 
-def deinfer_rope_store(q, k, v, positions, freqs, n_q_heads: int, n_kv_heads: int, head_dim: int, interleaved: bool = False,
-                       magnitude: float = 1.0, slots=None, q_out=None, k_out=None, v_out=None, stream=None):
-    """Queries rotated, keys rotated and values copied into their slots of the cache.  q, k and v may each be None; q_out, k_out
-    and v_out default to them (k and v: without slots only).  freqs: float64 device tensor [rot_dim / 2], or None to copy.  A row
-    whose slot is negative or behind the pools' last row is left out; with queries alone, one whose slot is negative."""
-    import torch
+def _store_args(q, k, v, q_out, k_out, v_out, slots, n_q_heads: int, n_kv_heads: int, head_dim: int):
+    """Rows and dtype of what is there of q, k and v, where each goes, the pools' rows, and pointer and pitch of each and of where it goes."""
     first = q if q is not None else k if k is not None else v
-    if first is None:
-        return q_out, k_out, v_out
     rows, dtype = (first.shape[0] if first.dim() else 0), first.dtype
     q_out = q if q_out is None else q_out
     if slots is None:
@@ -706,6 +709,18 @@ def deinfer_rope_store(q, k, v, positions, freqs, n_q_heads: int, n_kv_heads: in
             args.append((t.data_ptr(), ld, to.data_ptr(), ldo))
         if pooled:
             n_slots = to.shape[0] if n_slots is None else min(n_slots, to.shape[0])
+    return rows, first, q_out, k_out, v_out, (1 << 31 if n_slots is None else n_slots), args
+
+
+def deinfer_rope_store(q, k, v, positions, freqs, n_q_heads: int, n_kv_heads: int, head_dim: int, interleaved: bool = False,
+                       magnitude: float = 1.0, slots=None, q_out=None, k_out=None, v_out=None, stream=None):
+    """Queries rotated, keys rotated and values copied into their slots of the cache.  q, k and v may each be None; q_out, k_out
+    and v_out default to them (k and v: without slots only).  freqs: float64 device tensor [rot_dim / 2], or None to copy.  A row
+    whose slot is negative or behind the pools' last row is left out; with queries alone, one whose slot is negative."""
+    import torch
+    if q is None and k is None and v is None:
+        return q_out, k_out, v_out
+    rows, first, q_out, k_out, v_out, n_slots, args = _store_args(q, k, v, q_out, k_out, v_out, slots, n_q_heads, n_kv_heads, head_dim)
     if freqs is not None:
         if freqs.dtype != torch.float64 or not freqs.is_contiguous():
             raise ValueError("freqs: contiguous float64 tensor expected")
@@ -717,7 +732,7 @@ def deinfer_rope_store(q, k, v, positions, freqs, n_q_heads: int, n_kv_heads: in
     (qp, ldq, qo, ldqo), (kp, ldk, ko, ldko), (vp, ldv, vo, ldvo) = args
     _check(lib().deinfer_rope_store(qp, ldq, int(n_q_heads), kp, ldk, vp, ldv, int(n_kv_heads), rows, int(head_dim),
                                     0 if freqs is None else 2 * freqs.numel(), int(interleaved), _ptr(positions), _ptr(freqs), float(magnitude),
-                                    _ptr(slots), 1 << 31 if n_slots is None else n_slots, qo, ldqo, ko, ldko, vo, ldvo, _dtype_code(first), _stream(stream)))
+                                    _ptr(slots), n_slots, qo, ldqo, ko, ldko, vo, ldvo, _dtype_code(first), _stream(stream)))
     return q_out, k_out, v_out
 
 
@@ -761,4 +776,113 @@ def deinfer_tree_attention(q, k_pool, v_pool, block_table, row_start, cached, ws
                                         _ptr(mask), words, _ptr(k_pool), ldk, _ptr(v_pool), ldv, n_slots // int(block_tokens) if block_tokens > 0 else 0,
                                         int(block_tokens), _ptr(block_table), pitch, (head_dim or 1) ** -0.5 if scale is None else float(scale),
                                         _ptr(out), ldo, _dtype_code(q), _ptr(ws.buf), ws.nbytes, _stream(stream)))
+    return out
+
+
+# ------------------------------------------------------------------ between the projections of a prompt
+def deinfer_axis_positions(segments, segment_start, row_start, cached, rows: int, positions=None, stream=None):
+    """Positions [3, rows] (time, height, width) of a step's tokens, from their requests' segments: int32 [n_segments, 4], {t, h, w,
+    step}, h or w not positive for text of t tokens.  cached: tokens of each request before the step's (None: none).  Columns
+    behind the last sequence's keep what ``positions`` holds (a new one: whatever its memory held)."""
+    import torch
+    _ints("segments", segments)
+    if segments.dim() != 2 or segments.shape[1] != 4:
+        raise ValueError("segments: [n_segments, 4] expected")
+    _ints("segment_start", segment_start, 1)
+    n = segment_start.numel() - 1
+    _ints("row_start", row_start, n + 1)
+    if cached is not None:
+        _ints("cached", cached, n)
+    if positions is None:
+        positions, pitch = _new((3, int(rows)), torch.int32, row_start.device, stream), int(rows)
+    else:
+        have, cols, pitch = _matrix(positions, "positions")
+        if positions.dtype != torch.int32 or have < 3 or cols < rows:
+            raise ValueError("positions: int32 [3, rows] expected")
+    _on_device(segments, segment_start, row_start, cached, positions)
+    _check(lib().deinfer_axis_positions(_ptr(segments), segments.shape[0], _ptr(segment_start), _ptr(row_start), _ptr(cached), n, int(rows),
+                                        _ptr(positions), pitch, _stream(stream)))
+    return positions
+
+
+def deinfer_rope_axes(rot_dim: int, pairs: Sequence[int], turns: bool = False):
+    """The axis of every rotated pair (host): uint8 numpy [rot_dim / 2], from the number of pairs of each axis, axis after axis or
+    given out by turns."""
+    import numpy as np
+    axis_of = np.zeros(max(int(rot_dim), 2) // 2, dtype=np.uint8)
+    counts = (ctypes.c_int32 * max(len(pairs), 1))(*[int(n) for n in pairs])
+    _check(lib().deinfer_rope_axes(int(rot_dim), len(pairs), counts, int(turns), axis_of.ctypes.data_as(ctypes.POINTER(ctypes.c_uint8))))
+    return axis_of
+
+
+def deinfer_norm_rope_store(q, k, v, positions, freqs, n_q_heads: int, n_kv_heads: int, head_dim: int, q_weight=None, k_weight=None, eps: float = 1e-6,
+                            axis_of=None, interleaved: bool = False, magnitude: float = 1.0, slots=None, q_out=None, k_out=None, v_out=None, stream=None):
+    """``deinfer_rope_store`` with every head of q and k normed by its root mean square ahead of the rotation (where its weight
+    [head_dim] is given), and positions of several axes: int32 [n_axes, rows] with axis_of, uint8 device tensor [rot_dim / 2]."""
+    import torch
+    if q is None and k is None and v is None:
+        return q_out, k_out, v_out
+    rows, first, q_out, k_out, v_out, n_slots, args = _store_args(q, k, v, q_out, k_out, v_out, slots, n_q_heads, n_kv_heads, head_dim)
+    axes, pitch = 1, rows
+    if freqs is not None:
+        if freqs.dtype != torch.float64 or not freqs.is_contiguous():
+            raise ValueError("freqs: contiguous float64 tensor expected")
+        if freqs.numel() and positions is not None and positions.dim() == 2:
+            axes, cols, pitch = _matrix(positions, "positions")
+            if positions.dtype != torch.int32 or cols < rows:
+                raise ValueError("positions: int32 [n_axes, rows] expected")
+            if axes > 1 and (axis_of is None or axis_of.dtype != torch.uint8 or not axis_of.is_contiguous() or axis_of.numel() != freqs.numel()):
+                raise ValueError("axis_of: contiguous uint8 tensor with the axis of every pair expected")
+        elif freqs.numel():
+            _ints("positions", positions, rows)
+    for what, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None and (w.dtype != first.dtype or not w.is_contiguous() or w.numel() != head_dim):
+            raise ValueError(f"{what}: contiguous [head_dim] of the rows' dtype expected")
+    if slots is not None:
+        _ints("slots", slots, rows)
+    _on_device(q, k, v, positions, freqs, slots, q_weight, k_weight, axis_of if axes > 1 else None,
+               None if q_out is q or q is None else q_out, None if k_out is k or k is None else k_out, None if v_out is v or v is None else v_out)
+    (qp, ldq, qo, ldqo), (kp, ldk, ko, ldko), (vp, ldv, vo, ldvo) = args
+    _check(lib().deinfer_norm_rope_store(qp, ldq, int(n_q_heads), kp, ldk, vp, ldv, int(n_kv_heads), rows, int(head_dim),
+                                         0 if freqs is None else 2 * freqs.numel(), int(interleaved), _ptr(q_weight), _ptr(k_weight), float(eps),
+                                         _ptr(positions), pitch, axes, _ptr(axis_of) if axes > 1 else None, _ptr(freqs), float(magnitude),
+                                         _ptr(slots), n_slots, qo, ldqo, ko, ldko, vo, ldvo, _dtype_code(first), _stream(stream)))
+    return q_out, k_out, v_out
+
+
+def deinfer_prompt_attention_workspace_bytes(rows: int, n_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    n = _sz(0)
+    _check(lib().deinfer_prompt_attention_workspace_bytes(int(rows), int(n_seqs), int(n_q_heads), int(n_kv_heads), int(head_dim), ctypes.byref(n)))
+    return int(n.value)
+
+
+def deinfer_prompt_attention(q, k, v, q_start, ws: Workspace, n_q_heads: int, n_kv_heads: int, k_start=None, scale: Optional[float] = None, left: int = -1,
+                             right: int = 0, out=None, stream=None):
+    """Attention of packed sequences: q [rows, n_q_heads * head_dim]; k, v [key rows, n_kv_heads * head_dim]; q_start, k_start: int32
+    [n_seqs + 1] (k_start None: q_start).  A row sees the keys from ``left`` before its place to ``right`` behind it, the last row
+    standing at the last key; negative: no bound.  Rows behind the last sequence's keep what ``out`` holds (a new one:
+    whatever its memory held)."""
+    rows, cols, ldq = _matrix(q, "q")
+    _ints("q_start", q_start, 1)
+    n = q_start.numel() - 1
+    if n_q_heads <= 0 or cols % n_q_heads:
+        raise ValueError("q: [rows, n_q_heads * head_dim] expected")
+    head_dim, dtype = cols // n_q_heads, q.dtype
+    (n_keys, k_cols, ldk), (v_rows, v_cols, ldv) = _matrix(k, "k"), _matrix(v, "v")
+    if v_rows != n_keys or k_cols < n_kv_heads * head_dim or v_cols < n_kv_heads * head_dim:
+        raise ValueError("k, v: [key rows, n_kv_heads * head_dim] expected")
+    if k.dtype != dtype or v.dtype != dtype:
+        raise ValueError("q, k and v must share a dtype")
+    if k_start is not None:
+        _ints("k_start", k_start, n + 1)
+    if out is None:
+        out, ldo = _new((rows, cols), dtype, q.device, stream), max(cols, 1)
+    else:
+        out_rows, out_cols, ldo = _matrix(out, "out")
+        if out.dtype != dtype or out_rows < rows or out_cols < cols:
+            raise ValueError("out: [rows, n_q_heads * head_dim] of q's dtype expected")
+    _on_device(q, k, v, q_start, k_start, out, ws.buf)
+    _check(lib().deinfer_prompt_attention(_ptr(q), rows, ldq, int(n_q_heads), int(n_kv_heads), head_dim, _ptr(q_start), _ptr(k), ldk, _ptr(v), ldv, n_keys,
+                                          _ptr(k_start), n, int(left), int(right), (head_dim or 1) ** -0.5 if scale is None else float(scale),
+                                          _ptr(out), ldo, _dtype_code(q), _ptr(ws.buf), ws.nbytes, _stream(stream)))
     return out

@@ -32,8 +32,14 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found")
 
 
+# The wavefronts of the attention over packed keys that have 512 registers: matrix products with their sums in ordinary registers.
+# Left to itself the compiler puts them into accumulation registers and moves them back and forth around each
+# rescaling (heads of 256: 3060 moves and 21 registers in scratch memory, with the option 208 and none).
+SOURCE_FLAGS = {name: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for name in ("prompt_attention_bf16.hip", "prompt_attention_f16.hip")}
+
+
 def sources():
-    return [os.path.join(CSRC, "deinfer_api.hip"), os.path.join(CSRC, "cache_step_api.hip")]
+    return [os.path.join(CSRC, name + ".hip") for name in ("deinfer_api", "cache_step_api", "prompt_api", "prompt_attention_bf16", "prompt_attention_f16")]
 
 
 SAN_LIB = os.path.join(HERE, "libdeinfer_hostsan.so")
@@ -68,7 +74,7 @@ def build_library(verbose: bool = False, extra_flags=(), out: str = LIB, check_l
     flags = [hipcc(), *HIPCC_FLAGS, *extra_flags, "-I", os.path.join(os.path.dirname(HERE), "include")]
     with tempfile.TemporaryDirectory(prefix="deinfer_build_") as tmp:
         objects = [os.path.join(tmp, os.path.basename(src) + ".o") for src in sources()]
-        jobs = [[*flags, "-c", src, "-o", obj] for src, obj in zip(sources(), objects)]
+        jobs = [[*flags, *SOURCE_FLAGS.get(os.path.basename(src), ()), "-c", src, "-o", obj] for src, obj in zip(sources(), objects)]
         running = [subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True) for cmd in jobs]
         results = [(cmd, p.communicate()[1], p.returncode) for cmd, p in zip(jobs, running)]
         if all(rc == 0 for _, _, rc in results):

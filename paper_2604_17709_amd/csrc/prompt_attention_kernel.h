@@ -1,0 +1,860 @@
+// Attention of packed prompts over packed keys and values: rows of q, k and v as the projections write them (or keys
+// and values rebuilt from the low-rank cache), sequence after sequence, no pages.
+//
+// Token i of a sequence with n rows and K keys stands at p = K - n + i and sees the keys j with p - left <= j <= p + right,
+//   o = sum_j exp(x_j - max x) v_j / sum_j exp(x_j - max x),   x_j = scale q . k_j,
+// in one pass over the keys: a reference m, a running sum l and an unnormalised output O per row, all in fp32.
+//
+// A tile is `tile_tokens` tokens of a sequence with the query heads that share a key head: neighbouring heads use the same keys, so
+// a tile of grouped heads has few tokens and little beyond its diagonal.  Its keys [F, E) are those that some row of it sees.
+// Work is counted in keys of a tile, over all sequences, key heads and tiles, and START more per tile, what a tile costs beside
+// its keys; every workgroup takes an equal run, found on the device from the lengths: the sums over a sequence's tiles are those of
+// clamped arithmetic series, so the run is found by a scan over the sequences and a bisection.  A stage (UNIT keys) belongs to the
+// workgroup whose run its last key falls into.  A tile whose stages several workgroups share leaves partial (O, m, l) in
+// the workspace, at most two per workgroup, and a second launch joins them in order: results do not depend on timing.
+#pragma once
+#include "tree_attention_kernel.h"
+
+namespace deinfer {
+
+constexpr int PROMPT_FAR = 1 << 29;              // a window side without a bound
+
+struct PromptParams {
+  const uint16_t *q, *k, *v;
+  uint16_t *out;
+  const int *q_start, *k_start;
+  long long ldq, ldo;
+  uint32_t ldk, ldv;                             // in bytes
+  int T, Tk, n_seqs, head_dim, group;
+  int heads, head_tiles, tile_group, tile_tokens;      // key heads x parts of their query heads (head_tiles); query heads and tokens of a tile
+  int left, right;                               // at most PROMPT_FAR
+  float scale2;                                  // scale log2(e): the exponentials are powers of two
+  int n_shares;
+  float *part;                                   // [2 n_shares][rows][columns] partial outputs
+  float2 *part_ml;                               // [2 n_shares][rows] their references and sums
+  int4 *joins;                                   // [n_shares] tile whose first share this is and that others share (sequence, head, tile, shares)
+};
+
+struct PromptSeq { int row0, n, key0, keys; };
+__device__ __forceinline__ PromptSeq prompt_seq(const PromptParams &P, int s) {
+  auto range = [&](const int *start, int most, int &from, int &count) {
+    int a = start[s], b = start[s + 1];
+    a = a < 0 ? 0 : a; b = b > most ? most : b;
+    from = a; count = b > a ? b - a : 0;
+  };
+  PromptSeq q;
+  range(P.q_start, P.T, q.row0, q.n);
+  if (P.k_start) range(P.k_start, P.Tk, q.key0, q.keys);
+  else range(P.q_start, P.Tk < P.T ? P.Tk : P.T, q.key0, q.keys);
+  return q;
+}
+// keys of a tile: [first, first + count)
+struct PromptKeys { int first, count; };
+__device__ __forceinline__ PromptKeys prompt_keys(const PromptParams &P, const PromptSeq &q, int tile) {
+  const int c0 = q.keys - q.n, t0 = tile * P.tile_tokens;
+  const int t1 = q.n - t0 < P.tile_tokens ? q.n : t0 + P.tile_tokens;
+  int a = c0 + t0 - P.left, b = c0 + t1 + P.right;
+  a = a < 0 ? 0 : a > q.keys ? q.keys : a;
+  b = b < 0 ? 0 : b > q.keys ? q.keys : b;
+  return {a, b - a};
+}
+// sum over i < t of a + i step, each held within [0, most]
+__device__ __forceinline__ long long clamped_series(int a, int step, int most, int t) {
+  int z = a >= 0 ? 0 : (int)(((uint32_t)(-a) + (uint32_t)step - 1) / (uint32_t)step);
+  int f = a >= most ? 0 : (int)(((uint32_t)(most - a) + (uint32_t)step - 1) / (uint32_t)step);
+  z = z > t ? t : z; f = f > t ? t : f;
+  if (f <= z) return (long long)(t - f) * most;
+  return (long long)(f - z) * a + ((long long)f * (f - 1) - (long long)z * (z - 1)) / 2 * step + (long long)(t - f) * most;
+}
+// work of a sequence's first t tiles of one head
+template <int START> __device__ __forceinline__ long long prompt_work(const PromptParams &P, const PromptSeq &q, int t) {
+  const int c0 = q.keys - q.n, step = P.tile_tokens;
+  return (long long)t * START + clamped_series(c0 + step + P.right, step, q.keys, t) - clamped_series(c0 - P.left, step, q.keys, t);
+}
+__device__ __forceinline__ int prompt_tiles(const PromptParams &P, const PromptSeq &q) { return (q.n + P.tile_tokens - 1) / P.tile_tokens; }
+
+// A workgroup's run, tile after tile.  Everything is the same in all lanes.
+template <int UNIT, int START, int THREADS> struct PromptRun {
+  long long per_share, from_work, end, base;     // base: work ahead of the present tile's first key (behind its START)
+  PromptSeq seq;
+  int s, h, tile;
+  PromptKeys keys;
+  int k_from, k_to;                              // the workgroup's part of the present tile's keys, relative to keys.first
+
+  // scan: THREADS / 64 values, found: 2 values of LDS.  False: nothing to do
+  __device__ __forceinline__ bool begin(const PromptParams &P, int share, long long *scan, long long *found) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    auto work_of = [&](int x) -> long long {
+      if (x >= P.n_seqs) return 0;
+      const PromptSeq q = prompt_seq(P, x);
+      return P.heads * prompt_work<START>(P, q, prompt_tiles(P, q));
+    };
+    auto scan_work = [&](long long u, long long *total) {            // inclusive sum over the threads
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const long long w = __shfl_up(u, o, 64);
+        if (lane >= o) u += w;
+      }
+      __syncthreads();
+      if (lane == 63) scan[wave] = u;
+      __syncthreads();
+      long long all = 0, before = 0;
+      for (int w = 0; w < THREADS / 64; ++w) { if (w < wave) before += scan[w]; all += scan[w]; }
+      *total = all;
+      return u + before;
+    };
+    // (the last pass over up to THREADS sequences is kept: with no more of them there is one pass)
+    long long total = 0, mine = 0, mine_end = 0;
+    for (int s0 = 0; s0 < P.n_seqs; s0 += THREADS) {
+      long long t;
+      mine = work_of(s0 + tid);
+      mine_end = scan_work(mine, &t);
+      total += t;
+    }
+    total = uniform(total);
+    per_share = (total + P.n_shares - 1) / P.n_shares;
+    per_share = per_share < UNIT ? UNIT : per_share;                 // (every share between a tile's first and last then has a stage's last key)
+    from_work = per_share * share;
+    end = from_work + per_share < total ? from_work + per_share : total;
+    if (from_work >= end) return false;
+    long long before = 0;
+    for (int s0 = 0; s0 < P.n_seqs; s0 += THREADS) {
+      long long t = total;
+      if (P.n_seqs > THREADS) {
+        mine = work_of(s0 + tid);
+        mine_end = scan_work(mine, &t);
+      }
+      const long long e = before + mine_end;
+      if (mine > 0 && e - mine <= from_work && from_work < e) { found[0] = s0 + tid; found[1] = e - mine; }
+      before += t;
+      if (before > from_work) break;
+    }
+    __syncthreads();
+    s = __builtin_amdgcn_readfirstlane((int)found[0]);
+    base = uniform(found[1]);
+    seq = prompt_seq(P, s);
+    const long long per_head = uniform(prompt_work<START>(P, seq, prompt_tiles(P, seq)));
+    h = (int)((from_work - base) / per_head);
+    base += h * per_head;
+    int lo = 0, hi = prompt_tiles(P, seq) - 1;   // the last tile that begins at or before from_work
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (base + prompt_work<START>(P, seq, mid) <= from_work) lo = mid; else hi = mid - 1;
+    }
+    tile = __builtin_amdgcn_readfirstlane(lo);
+    base = uniform(base + prompt_work<START>(P, seq, tile) + START);
+    keys = prompt_keys(P, seq, tile);
+    part();
+    return mine_first() || next(P);
+  }
+  // the workgroup's keys of the present tile: whole stages from the tile's first key on, each of the share that its last key falls into
+  __device__ __forceinline__ void part() {
+    auto stages = [&](long long o) { return o <= 0 ? 0 : o >= keys.count ? keys.count : (int)o / UNIT * UNIT; };
+    k_from = stages(from_work - base); k_to = stages(end - base);
+  }
+  // a tile without keys is that of the share that its beginning falls into
+  __device__ __forceinline__ bool mine_first() const { return keys.count > 0 ? k_from < k_to : from_work <= base - START && base - START < end; }
+  // on to the next tile with keys (or rows to clear) of this workgroup
+  __device__ __forceinline__ bool next(const PromptParams &P) {
+    do {
+      base += keys.count + START;
+      if (base - START >= end) return false;
+      if ((tile + 1) * P.tile_tokens < seq.n) {
+        ++tile;
+      } else {
+        tile = 0;
+        if (++h == P.heads) {
+          h = 0;
+          do {
+            if (++s >= P.n_seqs) return false;
+            seq = prompt_seq(P, s);
+          } while (seq.n == 0);
+        }
+      }
+      keys = prompt_keys(P, seq, tile);
+      part();
+    } while (!mine_first());
+    return true;
+  }
+  // the workgroup has all of the present tile; it has its first keys
+  __device__ __forceinline__ bool whole() const { return k_from == 0 && k_to == keys.count; }
+  __device__ __forceinline__ bool first() const { return k_from == 0; }
+  // shares that have stages of the present tile
+  __device__ __forceinline__ int sharers() const {
+    const int one = keys.count < UNIT ? keys.count : UNIT;
+    return (int)((base + keys.count - 1) / per_share - (base + one - 1) / per_share + 1);
+  }
+};
+
+// A row of a tile: its token and query head; false: there is none.
+__device__ __forceinline__ bool prompt_row(const PromptParams &P, const PromptSeq &q, int tile, int h, int r, int &token, int &head) {
+  const int j = r / P.tile_group, g = r - j * P.tile_group, kv = h / P.head_tiles, g0 = (h - kv * P.head_tiles) * P.tile_group;
+  token = tile * P.tile_tokens + j;
+  head = kv * P.group + g0 + g;
+  return j < P.tile_tokens && token < q.n && g0 + g < P.group;
+}
+
+template <int ROWS> constexpr int PROMPT_START = ROWS == 16 ? 128 : 256;
+
+// ---- up to 16 rows per tile: single tokens and the like over long caches.  Four wavefronts, each its own 32 of 128 keys,
+// operands straight from memory into registers (the products and the way of V's operand are those of tree_attention_kernel).
+template <int DT, int DP, bool FULL>
+__global__ __launch_bounds__(ATT_THREADS) void prompt_rows_kernel(const PromptParams P) {
+  constexpr int WK = ATT_THREADS / 64, UNIT = ATT_KEYS * WK, ROWS = 16, START = PROMPT_START<16>;
+  constexpr int KS = DP / 32, VE = DP == 64 ? 4 : 8, NC = DP / (16 * VE), NF = NC * VE, VW = VE / 2, OP = DP + 4;
+  constexpr float LIFT = DT == DT_F16 ? 32768.0f : 1.0f;           // (as there: fp16's small numbers)
+  constexpr uint32_t ONES = DT == DT_F16 ? 0x3c003c00u : 0x3f803f80u;
+  __shared__ __attribute__((aligned(16))) float merge_o[WK * 16 * OP];
+  __shared__ float merge_ml[2 * WK * 16];
+  __shared__ long long scan[ATT_THREADS / 64];
+  __shared__ long long found[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, quarter = lane >> 4;
+  const int D = FULL ? DP : P.head_dim;
+  const int share = run_tile_of(blockIdx.x, P.n_shares);
+
+  PromptRun<UNIT, START, ATT_THREADS> run;
+  if (tid == 0) P.joins[share] = make_int4(-1, 0, 0, 0);
+  if (!run.begin(P, share, scan, found)) return;                   // (the same in every thread)
+  do {
+    const PromptSeq seq = run.seq;
+    const int s = run.s, h = run.h, tile = run.tile, kv = h / P.head_tiles;
+    int token, head;
+    const bool row = prompt_row(P, seq, tile, h, col, token, head);  // this lane's row
+    u32x4_t qf[KS];
+    {
+      const uint16_t *qp = P.q + (long long)(seq.row0 + token) * P.ldq + (long long)head * D + quarter * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        qf[ks] = u32x4_t{0u, 0u, 0u, 0u};
+        if (row && (FULL || ks * 32 + quarter * 8 < D)) qf[ks] = *reinterpret_cast<const u32x4_t *>(qp + ks * 32);
+      }
+    }
+    f32x4_t o[NF], l = {0.0f, 0.0f, 0.0f, 0.0f};
+    float m = -__builtin_inff();
+    const u32x4_t ones = {ONES, ONES, ONES, ONES};
+#pragma unroll
+    for (int f = 0; f < NF; ++f) o[f] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    // the keys that this lane's row sees: [low, high]; those that every row of the tile sees: [all_low, all_high]
+    const int place = seq.keys - seq.n + token, low = place - P.left, high = row ? place + P.right : -1;
+    const int t_last = (tile + 1) * P.tile_tokens < seq.n ? (tile + 1) * P.tile_tokens - 1 : seq.n - 1;
+    const int all_low = seq.keys - seq.n + t_last - P.left, all_high = seq.keys - seq.n + tile * P.tile_tokens + P.right;
+
+    const char *kh = reinterpret_cast<const char *>(P.k + (long long)kv * D) + (uint64_t)seq.key0 * P.ldk;
+    const char *vh = reinterpret_cast<const char *>(P.v + (long long)kv * D) + (uint64_t)seq.key0 * P.ldv;
+    const int k_last = run.keys.first + run.k_to;
+    for (int k0 = run.keys.first + run.k_from + wave * ATT_KEYS; k0 < k_last; k0 += UNIT) {
+      const uint32_t live = seq.keys - k0 >= 32 ? 0xffffffffu : (1u << (seq.keys - k0)) - 1u;        // the keys that exist
+      const bool whole = live == 0xffffffffu;
+      const char *kp = kh + (uint64_t)(uint32_t)k0 * P.ldk, *vp = vh + (uint64_t)(uint32_t)k0 * P.ldv;
+      auto held = [&](int x) { return whole || x < seq.keys - k0 ? x : seq.keys - k0 - 1; };          // (rows behind the last are not read)
+      u32x4_t kf[2][KS];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const char *kr = kp + (uint64_t)(uint32_t)held(16 * u + col) * P.ldk + quarter * 16;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          kf[u][ks] = u32x4_t{0u, 0u, 0u, 0u};
+          if (FULL || ks * 32 + quarter * 8 < D) kf[u][ks] = *reinterpret_cast<const u32x4_t *>(kr + ks * 64);
+        }
+      }
+      uint32_t vw[NC][8][VW];                    // [piece][key 4 u + i of the lane][word]
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const char *vr = vp + (uint64_t)(uint32_t)held(16 * (x / 4) + 4 * quarter + x % 4) * P.ldv + col * VE * 2;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+#pragma unroll
+          for (int w = 0; w < VW; ++w) vw[c][x][w] = 0u;
+          if (FULL || c * 16 * VE + col * VE < D) {
+            if constexpr (VE == 8) {
+              const u32x4_t t = *reinterpret_cast<const u32x4_t *>(vr + c * 256);
+#pragma unroll
+              for (int w = 0; w < 4; ++w) vw[c][x][w] = t[w];
+            } else {
+              const uint2 t = *reinterpret_cast<const uint2 *>(vr);
+              vw[c][x][0] = t.x; vw[c][x][1] = t.y;
+            }
+          }
+        }
+      }
+      const bool masked = !whole || k0 + 31 > all_high || k0 < all_low;
+      uint32_t sees = 0xffffffffu;               // of the 32 keys
+      bool odd_v = false;                        // a value that is infinite or NaN beside rows that do not see it
+      if (masked) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const bool there = (live >> (16 * (x / 4) + 4 * quarter + x % 4)) & 1u;
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int w = 0; w < VW; ++w) {
+              if (!there) vw[c][x][w] = 0u;
+              odd_v |= not_finite<DT>(vw[c][x][w]);
+            }
+        }
+        odd_v = __any(odd_v);
+        const int up = high - k0 + 1, down = low - k0;
+        sees = (up >= 32 ? 0xffffffffu : up <= 0 ? 0u : (1u << up) - 1u) & (down <= 0 ? 0xffffffffu : down >= 32 ? 0u : 0xffffffffu << down) & live;
+      }
+      f32x4_t sc[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        sc[u] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sc[u] = mfma16<DT>(kf[u][ks], qf[ks], sc[u]);
+      }
+      float p[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) p[x] = sc[x / 4][x % 4] * P.scale2;
+      if (masked) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          if (!((sees >> (16 * (x / 4) + 4 * quarter + x % 4)) & 1u)) p[x] = -__builtin_inff();
+      }
+      float top = p[0];
+#pragma unroll
+      for (int x = 1; x < 8; ++x) top = fmaxf(top, p[x]);
+      top = quarters_max(top);
+      if (__any(top > m)) {
+        const float m_new = fmaxf(m, top);
+        const float a = m == -__builtin_inff() ? 0.0f : att_exp2(m - m_new);
+        m = m_new;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) l[i] *= a;
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[f][i] *= a;
+      }
+      const float base = m == -__builtin_inff() ? 0.0f : m;        // (a row that has seen no key yet)
+#pragma unroll
+      for (int x = 0; x < 8; ++x) p[x] = att_exp2(p[x] - base) * LIFT;
+      // the probabilities, at most LIFT, as the 16-bit operand of the second product: each is off by at most half a step of the
+      // type, which is what the output's own rounding is off by; the sum is that of the rounded ones
+      const u32x4_t pf = {pack2<DT>(p[0], p[1]), pack2<DT>(p[2], p[3]), pack2<DT>(p[4], p[5]), pack2<DT>(p[6], p[7])};
+      l = mfma16<DT>(ones, pf, l);
+      if (!masked || !odd_v) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            u32x4_t vf;
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              vf[w] = __builtin_amdgcn_perm(vw[c][2 * w + 1][e / 2], vw[c][2 * w][e / 2], e % 2 ? 0x07060302u : 0x05040100u);
+            o[c * VE + e] = mfma16<DT>(vf, pf, o[c * VE + e]);
+          }
+      } else {
+        // 0 x infinity is no number: with such a value among the keys, every row adds up the keys that it sees, one by one
+#pragma unroll 1
+        for (int kk = 0; kk < 32; ++kk) {
+          if (!((live >> kk) & 1u)) continue;
+          const int x0 = 4 * (kk >> 4) + (kk & 3);
+          uint32_t w = pf[0];
+#pragma unroll
+          for (int x = 1; x < 4; ++x) w = (x0 >> 1) == x ? pf[x] : w;
+          const float mine = x0 & 1 ? hi_f32<DT>(w) : lo_f32<DT>(w);
+          const float pk = __shfl(mine, ((kk >> 2) & 3) * 16 + col, 64);
+          const bool see = (sees >> kk) & 1u;
+          const uint16_t *vr = reinterpret_cast<const uint16_t *>(vp + (uint64_t)(uint32_t)kk * P.ldv);
+#pragma unroll
+          for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int d = (f / VE) * 16 * VE + (quarter * 4 + i) * VE + f % VE;
+              if (see && (FULL || d < D)) o[f][i] += pk * cvt_in<DT>(vr[d]);
+            }
+        }
+      }
+    }
+
+    // ---- out: to the rows, where this workgroup had all their keys, else to the workspace
+    const bool whole = run.whole();
+    const long long which = 2LL * share + (run.first() ? 1 : 0);    // (a tile that begins here is the last of the run, one that does not the first)
+    __syncthreads();                                            // (the buffer's last readers are done)
+    if (quarter == 0) { merge_ml[(wave * 16 + col) * 2] = m; merge_ml[(wave * 16 + col) * 2 + 1] = l[0]; }
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float *mp = merge_o + (wave * 16 + col) * OP + c * 16 * VE + (quarter * 4 + i) * VE;
+#pragma unroll
+        for (int e = 0; e < VE; e += 4)
+          *reinterpret_cast<f32x4_t *>(mp + e) = f32x4_t{o[c * VE + e][i], o[c * VE + e + 1][i], o[c * VE + e + 2][i], o[c * VE + e + 3][i]};
+      }
+    __syncthreads();
+    for (int x = tid; x < 16 * (DP / VE); x += ATT_THREADS) {
+      const int rr = x / (DP / VE), d = (x - rr * (DP / VE)) * VE;
+      int t, hh;
+      if (!prompt_row(P, seq, tile, h, rr, t, hh) || (!FULL && d >= D)) continue;
+      float mm = merge_ml[rr * 2], ll = 0.0f, y[VE];
+#pragma unroll
+      for (int w = 1; w < WK; ++w) mm = fmaxf(mm, merge_ml[(w * 16 + rr) * 2]);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) y[e] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WK; ++w) {
+        // (a part without any key has l = 0 and O = 0, or, where all its scores were no numbers, neither: kept as it is)
+        const float mw = merge_ml[(w * 16 + rr) * 2], a = mw == -__builtin_inff() ? 1.0f : att_exp2(mw - mm);
+        ll += a * merge_ml[(w * 16 + rr) * 2 + 1];
+#pragma unroll
+        for (int e = 0; e < VE; ++e) y[e] += a * merge_o[(w * 16 + rr) * OP + d + e];
+      }
+      if (whole) {
+        uint16_t *op = P.out + (long long)(seq.row0 + t) * P.ldo + (long long)hh * D + d;
+        const float inv = ll > 0.0f || ll != ll ? 1.0f / ll : 0.0f;               // (no key seen: zeros)
+        uint32_t w[VW];
+#pragma unroll
+        for (int i = 0; i < VW; ++i) w[i] = pack2<DT>(y[2 * i] * inv, y[2 * i + 1] * inv);
+        if constexpr (VE == 8) *reinterpret_cast<u32x4_t *>(op) = u32x4_t{w[0], w[1], w[2], w[3]};
+        else *reinterpret_cast<uint2 *>(op) = make_uint2(w[0], w[1]);
+      } else {
+        float *pp = P.part + (which * ROWS + rr) * DP + d;
+#pragma unroll
+        for (int i = 0; i < VE; i += 4) *reinterpret_cast<f32x4_t *>(pp + i) = f32x4_t{y[i], y[i + 1], y[i + 2], y[i + 3]};
+        if (d == 0) P.part_ml[which * ROWS + rr] = make_float2(mm, ll);
+      }
+    }
+    if (!whole && run.first() && tid == 0) P.joins[share] = make_int4(s, h, tile, run.sharers());
+  } while (run.next(P));
+}
+
+// ---- more rows: WAVES wavefronts with RT times 32 rows each share the keys, STAGE at a time, through a ring of four stages in LDS.
+// KS: 16-feature steps of the first product (padded head dimension 16 KS); PITCH: features of a row in LDS.
+template <int KS_, int WAVES_, int RT_> struct PromptTile {
+  static constexpr int KS = KS_, WAVES = WAVES_, RT = RT_;
+  static constexpr int PITCH = KS <= 4 ? 64 : KS <= 8 ? 128 : 256;
+  static constexpr int NF = (KS + 1) / 2;        // 32-feature blocks of the output
+  static constexpr int STAGE = PITCH == 256 || (WAVES == 4 && RT == 1) ? 32 : 64;
+  static constexpr int PER_SIMD = WAVES == 4 && (PITCH == 256 || RT == 2) ? 1 : 2;           // wavefronts
+  static constexpr int THREADS = 64 * WAVES, ROWS = 32 * RT * WAVES, RING = 4;
+  static constexpr int ROWB = 2 * PITCH, BUF = STAGE * ROWB, LDS = RING * 2 * BUF;
+  static constexpr int COLS = 32 * NF;           // columns of a partial output
+};
+
+// The 16-byte pieces of a row in LDS are XORed with a number of the row's.  K: 32 rows at one piece are read 8 at a time, which
+// then cover all banks.  V: a transposing read takes 32 bytes of four neighbouring rows by 16 lanes, and with them in four different
+// groups of four pieces all banks are covered too.
+template <int PITCH> __device__ __forceinline__ int prompt_swizzle_k(int row) { return PITCH == 64 ? (row >> 1) & 7 : row & 15; }
+template <int PITCH> __device__ __forceinline__ int prompt_swizzle_v(int row) {
+  return PITCH == 64 ? (row & 2) << 1 : (row & 3) << 2 | ((row >> 2) & 3);
+}
+
+// c + both 16-bit values of a word
+template <int DT> __device__ __forceinline__ float add_pair(uint32_t w, float c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  if constexpr (DT == DT_F16) return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, w), __builtin_bit_cast(f16x2_t, 0x3c003c00u), c, false);
+  else return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), __builtin_bit_cast(bf16x2_t, 0x3f803f80u), c, false);
+#else
+  (void)w;
+  return c;
+#endif
+}
+
+template <int DT, int KS, int WAVES, int RT, bool FULL>
+__global__ __launch_bounds__(64 * WAVES, (PromptTile<KS, WAVES, RT>::PER_SIMD)) void prompt_tile_kernel(const PromptParams P) {
+  using C = PromptTile<KS, WAVES, RT>;
+  constexpr int ROWS = C::ROWS, STAGE = C::STAGE, THREADS = C::THREADS, NF = C::NF, ROWB = C::ROWB, BUF = C::BUF, START = PROMPT_START<ROWS>;
+  constexpr int CH = C::PITCH / 8;               // 16-byte pieces of a row
+  constexpr int WROWS = STAGE / WAVES;           // rows of K (of V) that a wavefront loads of a stage
+  constexpr int RPI = 64 / CH, NL = WROWS / RPI; // rows of one load instruction, load instructions
+  constexpr int HALVES = STAGE / 32;
+  constexpr float REF = DT == DT_F16 ? -12.0f : 16.0f, NONE = 3.402823466e38f, FAR = 16777216.0f;
+  static_assert(NL * RPI == WROWS, "whole load instructions");
+  extern __shared__ __attribute__((aligned(16))) unsigned char prompt_smem[];   // [RING][K, V][STAGE][ROWB]
+  __shared__ long long scan[THREADS / 64];
+  __shared__ long long found[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int D = FULL ? 16 * KS : P.head_dim;
+  const int share = run_tile_of(blockIdx.x, P.n_shares);
+  PromptRun<STAGE, START, THREADS> run;
+  if (tid == 0) P.joins[share] = make_int4(-1, 0, 0, 0);
+  if (!run.begin(P, share, scan, found)) return;                   // (the same in every thread)
+
+  // byte offset of this lane's operand of K in 32 rows, for the first step; for step ks its bits of 32 ks are the other way
+  const int kbase = col * ROWB + ((half ^ prompt_swizzle_k<C::PITCH>(col)) * 16);
+  // row (of 16: keys 4 half + ... and, 8 further, the same) that this lane addresses in a transposing read of V, and its 8 bytes there
+  const int vrow = 4 * half + ((lane & 15) >> 2), vpiece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+  const int vbase = vrow * ROWB + (lane & 1) * 8;
+
+  // The stages to be loaded run ahead of those in use, over the ends of tiles.
+  PromptRun<STAGE, START, THREADS> ahead = run;
+  int ahead_k = ahead.k_from;
+  bool more = true;
+  // The wavefront's rows of K and of V of the next stage into place b of the ring: 2 NL load instructions, whatever
+  // keys there are, so that the waits below can count them.  Keys that do not exist are rows of zeros.
+  auto issue = [&](int b) {
+    while (more && ahead_k >= ahead.k_to) {      // (tiles without keys have no stages)
+      more = ahead.next(P);
+      ahead_k = ahead.k_from;
+    }
+    unsigned char *kb = prompt_smem + b * 2 * BUF + wave * WROWS * ROWB, *vb = kb + BUF;
+    int ln = lane;
+    asm volatile("" : "+v"(ln));                 // (the few instructions anew each time: kept through the loop they cost registers)
+    auto row_of = [&](int i) { return ln / CH + RPI * i; };          // of the wavefront's rows
+    auto k_piece = [&](int i) { return (uint32_t)((ln % CH) ^ prompt_swizzle_k<C::PITCH>(WROWS * wave + row_of(i))); };
+    auto v_piece = [&](int i) { return (uint32_t)((ln % CH) ^ prompt_swizzle_v<C::PITCH>(WROWS * wave + row_of(i))); };
+    const int k0 = ahead.keys.first + ahead_k + WROWS * wave, kv = ahead.h / P.head_tiles;
+    const int left = more ? ahead.seq.keys - k0 : 0;                 // keys from the wavefront's first on
+    const uint64_t row0 = (uint32_t)(ahead.seq.key0 + k0);
+    const char *kr = reinterpret_cast<const char *>(P.k + (long long)kv * D) + row0 * P.ldk;
+    const char *vr = reinterpret_cast<const char *>(P.v + (long long)kv * D) + row0 * P.ldv;
+    if (FULL && 16 * KS == C::PITCH && left >= WROWS) {
+      settled(kr, vr);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        load_to_lds(kr, row_of(i) * P.ldk + k_piece(i) * 16, kb + i * 1024);
+        load_to_lds(vr, row_of(i) * P.ldv + v_piece(i) * 16, vb + i * 1024);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int r = row_of(i);
+        const uint32_t kp = k_piece(i), vp = v_piece(i);
+        const char *ka = kr + ((uint64_t)(uint32_t)r * P.ldk + kp * 16), *va = vr + ((uint64_t)(uint32_t)r * P.ldv + vp * 16);
+        load_to_lds(r < left && (int)kp * 8 < D ? ka : reinterpret_cast<const char *>(&att_zeros), kb + i * 1024);
+        load_to_lds(r < left && (int)vp * 8 < D ? va : reinterpret_cast<const char *>(&att_zeros), vb + i * 1024);
+      }
+    }
+    ahead_k += STAGE;
+  };
+  // the first KC operands of the 32 keys at kb (kx: kbase)
+  constexpr int KC = KS <= 8 ? KS : 4;
+  auto read_k = [&](const unsigned char *kb, int kx, u32x4_t (&kf)[KC]) {
+#pragma unroll
+    for (int ks = 0; ks < KC; ++ks) kf[ks] = *reinterpret_cast<const u32x4_t *>(kb + (kx ^ (ks * 32)));
+  };
+
+  issue(0); issue(1); issue(2);
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * NL) : "memory");
+  __builtin_amdgcn_s_barrier();                  // stage 0 has landed
+  asm volatile("" ::: "memory");
+  int b = 0;
+  do {
+    const PromptSeq seq = run.seq;
+    const int s = run.s, h = run.h, tile = run.tile;
+    u32x4_t qf[RT][KS];
+    int low[RT], high[RT];                       // keys that this lane's rows see
+    int all_low = -PROMPT_FAR, all_high = PROMPT_FAR;                // keys that every row of the wavefront sees
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      int token, head;
+      const bool row = prompt_row(P, seq, tile, h, (wave * RT + rt) * 32 + col, token, head);
+      const int place = seq.keys - seq.n + token;
+      low[rt] = place - P.left;
+      high[rt] = row ? place + P.right : -1;
+      const uint16_t *qp = P.q + (long long)(seq.row0 + token) * P.ldq + (long long)head * D + half * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        qf[rt][ks] = u32x4_t{0u, 0u, 0u, 0u};
+        if (row && (FULL || ks * 16 + half * 8 < D)) qf[rt][ks] = *reinterpret_cast<const u32x4_t *>(qp + ks * 16);
+      }
+    }
+    // (rows that are none see nothing and need no mask)
+    const int w0 = wave * RT * 32 / P.tile_group, w1 = (wave * RT * 32 + RT * 32 - 1) / P.tile_group;
+    const int t_first = tile * P.tile_tokens + w0;
+    int t_last = tile * P.tile_tokens + (w1 < P.tile_tokens ? w1 : P.tile_tokens - 1);
+    t_last = t_last < seq.n ? t_last : seq.n - 1;
+    const bool mine = w0 < P.tile_tokens && t_first < seq.n;         // the wavefront has rows
+    all_high = seq.keys - seq.n + t_first + P.right;
+    all_low = seq.keys - seq.n + t_last - P.left;
+    f32x16_t o[RT][NF];
+    float l[RT];                                 // of the lane's own keys: the half wave's other half has the rest
+    float ref[RT];                               // -m; NONE, fp32's largest number, where a row has seen no key yet: any score but minus infinity then makes an infinity
+    bool far_off = false;                        // some row's reference is FAR or more in size
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      ref[rt] = NONE; l[rt] = 0.0f;
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[rt][f][i] = 0.0f;
+    }
+    // scores of the 32 keys at kb, whose first operands are in kf
+    auto scores = [&](const unsigned char *kb, int kx, const u32x4_t (&kf)[KC], f32x16_t (&x)[RT]) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[rt][i] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const u32x4_t f = ks < KC ? kf[ks < KC ? ks : 0] : *reinterpret_cast<const u32x4_t *>(kb + (kx ^ (ks * 32)));
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) x[rt] = mfma32<DT>(f, qf[rt][ks], x[rt]);
+      }
+    };
+    const int k_first = run.keys.first + run.k_from, k_last = run.keys.first + run.k_to;
+    f32x16_t sc[RT];                             // scores of the next 32 keys
+    if (mine && k_first < k_last) {
+      u32x4_t kf[KC];
+      read_k(prompt_smem + b * 2 * BUF, kbase, kf);
+      scores(prompt_smem + b * 2 * BUF, kbase, kf, sc);
+    }
+    for (int k0 = k_first; k0 < k_last; k0 += STAGE, b = (b + 1) & 3) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * NL) : "memory");      // my rows of the next stage have landed
+      __builtin_amdgcn_s_barrier();                                                  // everybody's have; the stage before has been read
+      asm volatile("" ::: "memory");
+      issue((b + 3) & 3);
+      const unsigned char *kb = prompt_smem + b * 2 * BUF, *vb = kb + BUF, *kb_next = prompt_smem + ((b + 1) & 3) * 2 * BUF;
+      if (!mine) continue;
+      const bool masked = k0 + STAGE > seq.keys || k0 + STAGE - 1 > all_high || k0 < all_low;
+      bool odd_v = false;
+      if (masked) {                              // is there a value that is infinite or NaN?
+#pragma unroll 1
+        for (int x = 0; x < BUF / 1024; ++x) {
+          const u32x4_t v = *reinterpret_cast<const u32x4_t *>(vb + x * 1024 + lane * 16);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) odd_v |= not_finite<DT>(v[w]);
+        }
+        odd_v = __any(odd_v);
+      }
+#pragma unroll
+      for (int c = 0; c < HALVES; ++c) {         // 32 keys
+        int kx = kbase, vx = vbase, vz = vpiece ^ prompt_swizzle_v<C::PITCH>(vrow), hf = 4 * half;
+        asm volatile("" : "+v"(kx), "+v"(vx), "+v"(vz), "+v"(hf));      // (what is made of these is not kept through the loop)
+        const unsigned char *kn = c + 1 < HALVES ? kb + (c + 1) * 32 * ROWB : kb_next;      // the 32 keys after these
+        u32x4_t kf[KC];
+        read_k(kn, kx, kf);
+        auto sees = [&](int rt, int i) {         // key 8 (i / 4) + 4 half + i % 4 of the 32
+          const int at = 8 * (i / 4) + i % 4, up = high[rt] - (k0 + 32 * c) - hf, down = low[rt] - (k0 + 32 * c) - hf;
+          const int end = seq.keys - 1 - (k0 + 32 * c) - hf;
+          return at <= up && at >= down && at <= end;
+        };
+        auto hide = [&](f32x16_t (&x)[RT]) {
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (!sees(rt, i)) x[rt][i] = -__builtin_inff();
+        };
+        if (masked) hide(sc);
+        // ---- probabilities of these keys (rounded to the type: off by at most half a step, which is what the
+        // output's own rounding is off by), beside the scores of the next
+        u32x4_t pf[RT][2];
+        uint32_t any = 0;
+        auto probabilities = [&](const f32x16_t (&x)[RT]) {
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+              float p[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) p[e] = att_exp2(fmaf(x[rt][i + e], P.scale2, ref[rt]));
+              const uint32_t lo = pack2<DT>(p[0], p[1]), hi = pack2<DT>(p[2], p[3]);
+              pf[rt][i / 8][(i % 8) / 2] = lo; pf[rt][i / 8][(i % 8) / 2 + 1] = hi;
+              any = att_larger<DT>(any, lo, hi);
+            }
+        };
+        probabilities(sc);
+        scores(kn, kx, kf, sc);
+        if (__any(att_large<DT>(any)) || far_off) {
+          f32x16_t x[RT];
+          {
+            u32x4_t kr[KC];
+            read_k(kb + c * 32 * ROWB, kx, kr);
+            scores(kb + c * 32 * ROWB, kx, kr, x);
+          }
+          if (masked) hide(x);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            float top = x[rt][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, x[rt][i]);
+            top = fmaxf(top, __shfl_xor(top, 32, 64)) * P.scale2;
+            // The fused product above has more bits than the rounded one that the reference is made of: beside a reference of 2^24 (FAR)
+            // the difference is a factor of up to 2, beside one of 2^31 an infinity or nothing.  From FAR on the wavefront rounds the
+            // products, takes the maximum of every 32 keys, and a row's largest probability is 1.
+            const bool seen = top != -__builtin_inff(), far = seen && fabsf(top) >= FAR;
+            far_off |= __any(far) != 0;
+            const float ref_new = !seen ? ref[rt] : fminf(ref[rt], far ? -top : -(top + REF));
+            const float a = att_exp2(ref_new - ref[rt]);       // (0 from NONE on)
+            ref[rt] = ref_new;
+            l[rt] *= a;
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[rt][f][i] *= a;
+          }
+          if (far_off) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+              for (int i = 0; i < 16; i += 2) {
+                float p[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  float t = x[rt][i + e] * P.scale2;
+                  asm volatile("" : "+v"(t));    // (not fused with the sum)
+                  p[e] = att_exp2(t + ref[rt]);
+                }
+                pf[rt][i / 8][(i % 8) / 2] = pack2<DT>(p[0], p[1]);
+              }
+          } else {
+            probabilities(x);
+          }
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int x = 0; x < 8; ++x) l[rt] = add_pair<DT>(pf[rt][x / 4][x % 4], l[rt]);
+        if (!odd_v) {
+#pragma unroll
+          for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {     // keys 16 kk .. 16 kk + 15
+              uint2 v[2];
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {      // rows 8 u + vrow: their swizzle is that of vrow with the bits of 8 u the other way
+                const int row8 = 32 * c + 16 * kk + 8 * u;
+                v[u] = read_transposed(vb + row8 * ROWB + vx + (((f * 4) ^ vz ^ prompt_swizzle_v<C::PITCH>(8 * u)) * 16));
+              }
+              const u32x4_t vf = {v[0].x, v[0].y, v[1].x, v[1].y};
+#pragma unroll
+              for (int rt = 0; rt < RT; ++rt) o[rt][f] = mfma32<DT>(vf, pf[rt][kk], o[rt][f]);
+            }
+        } else {
+          // 0 x infinity is no number: with such a value among the keys, every row adds up the keys that it sees, one by one
+#pragma unroll 1
+          for (int kk = 0; kk < 32; ++kk) {
+            const int i0 = 4 * (kk >> 3) + (kk & 3);       // which of the lane's sixteen probabilities, of the half (kk >> 2) & 1
+            float pk[RT];
+            bool see[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+              uint32_t w = 0;
+#pragma unroll
+              for (int x = 0; x < 8; ++x) w |= (i0 >> 1) == x ? pf[rt][x / 4][x % 4] : 0u;
+              pk[rt] = __shfl(i0 & 1 ? hi_f32<DT>(w) : lo_f32<DT>(w), ((kk >> 2) & 1) * 32 + col, 64);
+              const int key = k0 + 32 * c + kk;
+              see[rt] = key <= high[rt] && key >= low[rt] && key < seq.keys;
+            }
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+              for (int g = 0; g < 4; ++g) {      // features 32 f + 8 g + 4 half .. + 3
+                int hh = half;
+                asm volatile("" : "+v"(hh));     // (an address of its own each time)
+                const int row = 32 * c + kk, piece = (4 * f + g) ^ prompt_swizzle_v<C::PITCH>(row);
+                const uint2 v = *reinterpret_cast<const uint2 *>(vb + row * ROWB + piece * 16 + hh * 8);
+                const float x[4] = {lo_f32<DT>(v.x), hi_f32<DT>(v.x), lo_f32<DT>(v.y), hi_f32<DT>(v.y)};
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                  if (see[rt]) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[rt][f][4 * g + i] += pk[rt] * x[i];
+                  }
+              }
+          }
+        }
+      }
+    }
+
+    // ---- out: to the rows, where this workgroup had all their keys, else to the workspace
+    const bool whole = run.whole();
+    const long long which = 2LL * share + (run.first() ? 1 : 0);
+    if (mine)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const int r = (wave * RT + rt) * 32 + col;
+        const float ll = l[rt] + __shfl_xor(l[rt], 32, 64);
+        int token, head;
+        if (!prompt_row(P, seq, tile, h, r, token, head)) continue;
+        if (whole) {
+          uint16_t *op = P.out + (long long)(seq.row0 + token) * P.ldo + (long long)head * D + 4 * half;
+          const float inv = ll > 0.0f || ll != ll ? 1.0f / ll : 0.0f;             // (no key seen: zeros)
+#pragma unroll
+          for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+              if ((FULL && KS % 2 == 0) || 32 * f + 8 * g < D)
+                *reinterpret_cast<uint2 *>(op + 32 * f + 8 * g) =
+                    make_uint2(pack2<DT>(o[rt][f][4 * g] * inv, o[rt][f][4 * g + 1] * inv), pack2<DT>(o[rt][f][4 * g + 2] * inv, o[rt][f][4 * g + 3] * inv));
+        } else {
+          float *pp = P.part + (which * ROWS + r) * C::COLS + 4 * half;
+#pragma unroll
+          for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+              *reinterpret_cast<f32x4_t *>(pp + 32 * f + 8 * g) = f32x4_t{o[rt][f][4 * g], o[rt][f][4 * g + 1], o[rt][f][4 * g + 2], o[rt][f][4 * g + 3]};
+          if (half == 0) P.part_ml[which * ROWS + r] = make_float2(ref[rt] == NONE ? -__builtin_inff() : -ref[rt], ll);
+        }
+      }
+    if (!whole && run.first() && tid == 0) P.joins[share] = make_int4(s, h, tile, run.sharers());
+  } while (run.next(P));
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (rows loaded ahead and not used: their place in LDS is this workgroup's until they land)
+}
+
+// Joins the partial results of the tiles whose keys several workgroups had: workgroup (b, y) takes sixteen rows of the tile that
+// begins in share b, whose other parts are the first of the shares after it.  Threads: (group of parts) x (row, 4
+// features); the groups' sums are joined in LDS in a fixed order.
+template <int DT, int COLS, int ROWS>
+__global__ __launch_bounds__(ROWS == 16 ? 1024 : 256) void prompt_join_kernel(const PromptParams P) {
+  const int share = blockIdx.x;
+  const int4 job = P.joins[share];
+  if (job.x < 0) return;
+  constexpr int THREADS = ROWS == 16 ? 1024 : 256, QUADS = COLS / 4, SETS = ROWS == 16 ? THREADS / (16 * QUADS) : 1, AHEAD = ROWS == 16 ? 4 : 2;
+  static_assert(SETS == 1 || SETS * 16 * QUADS == THREADS, "whole groups");
+  __shared__ __attribute__((aligned(16))) float sum_o[SETS > 1 ? SETS * 16 * COLS : 4];
+  __shared__ float sum_l[SETS > 1 ? SETS * 16 : 1];
+  const PromptSeq seq = prompt_seq(P, job.x);
+  const int h = job.y, tile = job.z, parts = job.w, tid = threadIdx.x, r0 = blockIdx.y * 16;
+  auto part_at = [&](int i, int r) -> long long { return ((long long)(2 * (share + i)) + (i == 0 ? 1 : 0)) * ROWS + r; };
+  for (int x = tid; x < SETS * 16 * QUADS; x += THREADS) {
+    const int set = x / (16 * QUADS), item = x - set * 16 * QUADS, rr = item / QUADS, d = (item - rr * QUADS) * 4, r = r0 + rr;
+    int token, head;
+    const bool row = prompt_row(P, seq, tile, h, r, token, head);
+    float mm = -__builtin_inff(), ll = 0.0f;
+    f32x4_t y = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (row) {
+      // (AHEAD loads side by side: the last part stands in for those behind it, and is not added)
+      for (int i0 = 0; i0 < parts; i0 += 2 * AHEAD) {
+        float t[2 * AHEAD];
+#pragma unroll
+        for (int i = 0; i < 2 * AHEAD; ++i) t[i] = P.part_ml[part_at(i0 + i < parts ? i0 + i : parts - 1, r)].x;
+#pragma unroll
+        for (int i = 0; i < 2 * AHEAD; ++i) mm = fmaxf(mm, t[i]);
+      }
+      for (int i0 = set; i0 < parts; i0 += SETS * AHEAD) {
+        float2 ml[AHEAD];
+        f32x4_t z[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          const long long at = part_at(i0 + SETS * i < parts ? i0 + SETS * i : parts - 1, r);
+          ml[i] = P.part_ml[at];
+          z[i] = *reinterpret_cast<const f32x4_t *>(P.part + at * COLS + d);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          if (i0 + SETS * i >= parts) continue;
+          const float a = ml[i].x == -__builtin_inff() ? 1.0f : att_exp2(ml[i].x - mm);
+          ll += a * ml[i].y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] += a * z[i][e];
+        }
+      }
+    }
+    if constexpr (SETS > 1) {
+      *reinterpret_cast<f32x4_t *>(sum_o + (set * 16 + rr) * COLS + d) = y;
+      if (d == 0) sum_l[set * 16 + rr] = ll;
+      __syncthreads();                                          // (one pass of the loop)
+      if (set == 0) {
+        ll = 0.0f; y = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < SETS; ++w) {
+          ll += sum_l[w * 16 + rr];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] += sum_o[(w * 16 + rr) * COLS + d + e];
+        }
+      }
+    }
+    if (set == 0 && row && d < P.head_dim) {
+      const float inv = ll > 0.0f || ll != ll ? 1.0f / ll : 0.0f;
+      *reinterpret_cast<uint2 *>(P.out + (long long)(seq.row0 + token) * P.ldo + (long long)head * P.head_dim + d) =
+          make_uint2(pack2<DT>(y[0] * inv, y[1] * inv), pack2<DT>(y[2] * inv, y[3] * inv));
+    }
+  }
+}
+
+}  // namespace deinfer
