@@ -43,7 +43,7 @@ PromptPlan prompt_plan(int64_t T, int64_t n_seqs, int64_t n_q, int64_t n_kv, int
   p.rows = per_head <= 16 ? 16 : head_dim > 128 || per_head <= 128 ? 128 : 256;
   p.cols = p.rows == 16 ? (head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256) : head_dim <= 64 ? 64 : head_dim <= 96 ? 96 : head_dim <= 128 ? 128 : 256;
   const int cus = device_cus();
-  p.shares = (p.rows == 16 || (p.rows == 128 && head_dim <= 128) ? 2 : 1) * (int64_t)(cus > 0 ? cus : 256);
+  p.shares = (p.rows == 16 ? 2 : 1) * (int64_t)(cus > 0 ? cus : 256);
   p.joins = PROMPT_WS_HEADER;
   p.ml = p.joins + (size_t)round_up(2 * (cus > 0 ? cus : 256) * 16, 256);           // (the same for every choice: more rows never need less)
   p.part = p.ml + (size_t)round_up(2 * p.shares * p.rows * 8, 256);

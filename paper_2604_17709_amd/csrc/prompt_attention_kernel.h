@@ -420,18 +420,20 @@ __global__ __launch_bounds__(ATT_THREADS) void prompt_rows_kernel(const PromptPa
   } while (run.next(P));
 }
 
-// ---- more rows: WAVES wavefronts with RT times 32 rows each share the keys, STAGE at a time, through a ring of four stages in LDS.
+// ---- more rows: WAVES wavefronts with 32 rows each share the keys, SLOT at a time, through a ring of four slots in LDS.
 // KS: 16-feature steps of the first product (padded head dimension 16 KS); PITCH: features of a row in LDS.
-template <int KS_, int WAVES_, int RT_> struct PromptTile {
-  static constexpr int KS = KS_, WAVES = WAVES_, RT = RT_;
+template <int KS_, int WAVES_> struct PromptTile {
+  static constexpr int KS = KS_, WAVES = WAVES_;
   static constexpr int PITCH = KS <= 4 ? 64 : KS <= 8 ? 128 : 256;
   static constexpr int NF = (KS + 1) / 2;        // 32-feature blocks of the output
-  static constexpr int STAGE = PITCH == 256 || (WAVES == 4 && RT == 1) ? 32 : 64;
-  static constexpr int PER_SIMD = WAVES == 4 && (PITCH == 256 || RT == 2) ? 1 : 2;           // wavefronts
-  static constexpr int THREADS = 64 * WAVES, ROWS = 32 * RT * WAVES, RING = 4;
-  static constexpr int ROWB = 2 * PITCH, BUF = STAGE * ROWB, LDS = RING * 2 * BUF;
+  static constexpr int SLOT = PITCH == 256 ? 32 : 64;
+  static constexpr int THREADS = 64 * WAVES, ROWS = 32 * WAVES, RING = 4;
+  static constexpr int ROWB = 2 * PITCH, BUF = SLOT * ROWB, LDS = RING * 2 * BUF;
   static constexpr int COLS = 32 * NF;           // columns of a partial output
 };
+constexpr int PROMPT_UNIT = 64;                  // keys of two steps of a wavefront
+
+__device__ const u32x4_t prompt_zeros[32] = {};  // a row of zeros
 
 // The 16-byte pieces of a row in LDS are XORed with a number of the row's.  K: 32 rows at one piece are read 8 at a time, which
 // then cover all banks.  V: a transposing read takes 32 bytes of four neighbouring rows by 16 lanes, and with them in four different
@@ -452,337 +454,406 @@ template <int DT> __device__ __forceinline__ float add_pair(uint32_t w, float c)
 #endif
 }
 
-template <int DT, int KS, int WAVES, int RT, bool FULL>
-__global__ __launch_bounds__(64 * WAVES, (PromptTile<KS, WAVES, RT>::PER_SIMD)) void prompt_tile_kernel(const PromptParams P) {
-  using C = PromptTile<KS, WAVES, RT>;
-  constexpr int ROWS = C::ROWS, STAGE = C::STAGE, THREADS = C::THREADS, NF = C::NF, ROWB = C::ROWB, BUF = C::BUF, START = PROMPT_START<ROWS>;
+// load_to_lds with LDS addresses as numbers
+__device__ __forceinline__ void load_to_lds_at(const void *from, uint32_t offset, uint32_t to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(from) : "memory", "m0");
+#else
+  (void)from; (void)offset; (void)to;
+#endif
+}
+__device__ __forceinline__ void load_to_lds_at(const void *from, uint32_t to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+#else
+  (void)from; (void)to;
+#endif
+}
+// pairs of 16-bit numbers: the larger, the smaller, the product's low halves, the difference or 0
+typedef unsigned short pair_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t larger_pair(uint32_t a, uint32_t b) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(pair_t, a), __builtin_bit_cast(pair_t, b))); }
+__device__ __forceinline__ uint32_t smaller_pair(uint32_t a, uint32_t b) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(pair_t, a), __builtin_bit_cast(pair_t, b))); }
+__device__ __forceinline__ uint32_t times_pair(uint32_t a, uint32_t b) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(pair_t, a) * __builtin_bit_cast(pair_t, b)); }
+__device__ __forceinline__ uint32_t minus_pair(uint32_t a, uint32_t b) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(pair_t, a), __builtin_bit_cast(pair_t, b))); }
+
+template <int DT, int KS, int WAVES, bool FULL>
+__global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(const PromptParams P) {
+  using C = PromptTile<KS, WAVES>;
+  constexpr int ROWS = C::ROWS, SLOT = C::SLOT, THREADS = C::THREADS, NF = C::NF, ROWB = C::ROWB, BUF = C::BUF, START = PROMPT_START<ROWS>;
   constexpr int CH = C::PITCH / 8;               // 16-byte pieces of a row
-  constexpr int WROWS = STAGE / WAVES;           // rows of K (of V) that a wavefront loads of a stage
+  constexpr int WROWS = SLOT / WAVES;            // rows of K (of V) that a wavefront loads of a slot
   constexpr int RPI = 64 / CH, NL = WROWS / RPI; // rows of one load instruction, load instructions
-  constexpr int HALVES = STAGE / 32;
   constexpr float REF = DT == DT_F16 ? -12.0f : 16.0f, NONE = 3.402823466e38f, FAR = 16777216.0f;
   static_assert(NL * RPI == WROWS, "whole load instructions");
-  extern __shared__ __attribute__((aligned(16))) unsigned char prompt_smem[];   // [RING][K, V][STAGE][ROWB]
+  extern __shared__ __attribute__((aligned(16))) unsigned char prompt_smem[];   // [RING][K, V][SLOT][ROWB]
   __shared__ long long scan[THREADS / 64];
   __shared__ long long found[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int D = FULL ? 16 * KS : P.head_dim;
   const int share = run_tile_of(blockIdx.x, P.n_shares);
-  PromptRun<STAGE, START, THREADS> run;
-  if (tid == 0) P.joins[share] = make_int4(-1, 0, 0, 0);
-  if (!run.begin(P, share, scan, found)) return;                   // (the same in every thread)
+  // Where the wavefront is in its run, and where its loads are, ahead of that: in LDS, so that the loop has the scalar registers.
+  using Run = PromptRun<PROMPT_UNIT, START, THREADS>;
+  __shared__ Run kept[2][WAVES];
+  {
+    Run run;
+    if (tid == 0) P.joins[share] = make_int4(-1, 0, 0, 0);
+    if (!run.begin(P, share, scan, found)) return;                 // (the same in every thread)
+    kept[0][wave] = run; kept[1][wave] = run;
+  }
+  auto advance = [&](int which) __attribute__((always_inline)) -> bool {
+    Run run = kept[which][wave];
+    const bool more = __builtin_amdgcn_readfirstlane(run.next(P));
+    kept[which][wave] = run;
+    return more;
+  };
+  auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
 
   // byte offset of this lane's operand of K in 32 rows, for the first step; for step ks its bits of 32 ks are the other way
   const int kbase = col * ROWB + ((half ^ prompt_swizzle_k<C::PITCH>(col)) * 16);
   // row (of 16: keys 4 half + ... and, 8 further, the same) that this lane addresses in a transposing read of V, and its 8 bytes there
-  const int vrow = 4 * half + ((lane & 15) >> 2), vpiece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+  const int vrow = 4 * half + ((lane & 15) >> 2), vpiece = (((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ prompt_swizzle_v<C::PITCH>(vrow);
   const int vbase = vrow * ROWB + (lane & 1) * 8;
 
-  // The stages to be loaded run ahead of those in use, over the ends of tiles.
-  PromptRun<STAGE, START, THREADS> ahead = run;
-  int ahead_k = ahead.k_from;
-  bool more = true;
-  // The wavefront's rows of K and of V of the next stage into place b of the ring: 2 NL load instructions, whatever
-  // keys there are, so that the waits below can count them.  Keys that do not exist are rows of zeros.
-  auto issue = [&](int b) {
-    while (more && ahead_k >= ahead.k_to) {      // (tiles without keys have no stages)
-      more = ahead.next(P);
-      ahead_k = ahead.k_from;
-    }
-    unsigned char *kb = prompt_smem + b * 2 * BUF + wave * WROWS * ROWB, *vb = kb + BUF;
-    int ln = lane;
-    asm volatile("" : "+v"(ln));                 // (the few instructions anew each time: kept through the loop they cost registers)
-    auto row_of = [&](int i) { return ln / CH + RPI * i; };          // of the wavefront's rows
-    auto k_piece = [&](int i) { return (uint32_t)((ln % CH) ^ prompt_swizzle_k<C::PITCH>(WROWS * wave + row_of(i))); };
-    auto v_piece = [&](int i) { return (uint32_t)((ln % CH) ^ prompt_swizzle_v<C::PITCH>(WROWS * wave + row_of(i))); };
-    const int k0 = ahead.keys.first + ahead_k + WROWS * wave, kv = ahead.h / P.head_tiles;
-    const int left = more ? ahead.seq.keys - k0 : 0;                 // keys from the wavefront's first on
-    const uint64_t row0 = (uint32_t)(ahead.seq.key0 + k0);
-    const char *kr = reinterpret_cast<const char *>(P.k + (long long)kv * D) + row0 * P.ldk;
-    const char *vr = reinterpret_cast<const char *>(P.v + (long long)kv * D) + row0 * P.ldv;
-    if (FULL && 16 * KS == C::PITCH && left >= WROWS) {
-      settled(kr, vr);
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        load_to_lds(kr, row_of(i) * P.ldk + k_piece(i) * 16, kb + i * 1024);
-        load_to_lds(vr, row_of(i) * P.ldv + v_piece(i) * 16, vb + i * 1024);
+  // The slots to be loaded run ahead of those in use, over the ends of tiles.  Of the next one: the wavefront's first row of K and of
+  // V, and how far behind it (in bytes) the sequence's last key is.  Rows behind the last key are that key's again: nothing sees them.
+  const char *kr = reinterpret_cast<const char *>(prompt_zeros), *vr = kr;
+  uint32_t k_most = 0, v_most = 0;
+  int steady = 0, after = -1;                    // slots to come that only move on; where in the tile's keys the one behind them begins
+  bool over = false;
+  auto another_slot = [&]() __attribute__((always_inline)) {
+    steady = 0;
+    if (over) return;
+    if (after < 0) after = scalar(kept[1][wave].k_from);
+    while (after >= scalar(kept[1][wave].k_to)) {                  // (tiles without keys have no slots)
+      if (!advance(1)) {                         // no slot is left: rows of zeros, which nothing reads
+        over = true;
+        kr = vr = reinterpret_cast<const char *>(prompt_zeros);
+        k_most = v_most = 0;
+        return;
       }
+      after = scalar(kept[1][wave].k_from);
+    }
+    const Run &at = kept[1][wave];
+    const int kv = scalar(at.h) / P.head_tiles, keys = scalar(at.seq.keys), k0 = scalar(at.keys.first) + after + WROWS * wave, k_to = scalar(at.k_to);
+    const int rest = keys - k0;                  // keys from the wavefront's first row on
+    const uint32_t row0 = scalar(at.seq.key0) + (rest > 0 ? k0 : keys - 1);
+    kr = reinterpret_cast<const char *>(P.k + (long long)kv * D) + (uint64_t)row0 * P.ldk;
+    vr = reinterpret_cast<const char *>(P.v + (long long)kv * D) + (uint64_t)row0 * P.ldv;
+    k_most = v_most = 0xffffffffu;
+    int here = 1;
+    if (rest < WROWS) {
+      const uint32_t last = rest > 0 ? rest - 1 : 0;
+      k_most = last * P.ldk; v_most = last * P.ldv;
     } else {
+      const int whole = (rest - WROWS) / SLOT + 1, left = (k_to - after + PROMPT_UNIT - 1) / PROMPT_UNIT * PROMPT_UNIT / SLOT;
+      here = whole < left ? whole : left;
+    }
+    steady = here - 1;
+    after += here * SLOT;
+  };
+  auto next_slot = [&]() __attribute__((always_inline)) {
+    if (__builtin_expect(steady > 0, 1)) {
+      --steady;
+      kr += (uint64_t)SLOT * P.ldk; vr += (uint64_t)SLOT * P.ldv;
+    } else {
+      another_slot();
+    }
+  };
+  // This lane's part of a load instruction: its row (in bytes) and its piece; those of instruction i are RPI i rows further on.
+  const uint32_t k_row = (lane / CH) * P.ldk, v_row = (lane / CH) * P.ldv;
+  const uint32_t k_off = ((lane % CH) ^ prompt_swizzle_k<C::PITCH>(WROWS * wave + lane / CH)) * 16, v_off = ((lane % CH) ^ prompt_swizzle_v<C::PITCH>(WROWS * wave + lane / CH)) * 16;
+  const uint32_t ring = lds_at(prompt_smem) + wave * WROWS * ROWB;             // the wavefront's rows of the ring's first place
+  // Its rows into place b of the ring: 2 NL load instructions, whatever keys there are, so that the waits below can count them.
+  auto issue = [&](int b) __attribute__((always_inline)) {
+    const uint32_t kb = ring + b * 2 * BUF, vb = kb + BUF;
+    const char *ks = kr, *vs = vr;
+    settled(ks, vs);
 #pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const int r = row_of(i);
-        const uint32_t kp = k_piece(i), vp = v_piece(i);
-        const char *ka = kr + ((uint64_t)(uint32_t)r * P.ldk + kp * 16), *va = vr + ((uint64_t)(uint32_t)r * P.ldv + vp * 16);
-        load_to_lds(r < left && (int)kp * 8 < D ? ka : reinterpret_cast<const char *>(&att_zeros), kb + i * 1024);
-        load_to_lds(r < left && (int)vp * 8 < D ? va : reinterpret_cast<const char *>(&att_zeros), vb + i * 1024);
+    for (int i = 0; i < NL; ++i) {
+      uint32_t k_at = k_row + RPI * i * P.ldk, v_at = v_row + RPI * i * P.ldv;
+      const uint32_t kp = k_off ^ (prompt_swizzle_k<C::PITCH>(RPI * i) * 16), vp = v_off ^ (prompt_swizzle_v<C::PITCH>(RPI * i) * 16);
+      k_at = (k_at < k_most ? k_at : k_most) + kp; v_at = (v_at < v_most ? v_at : v_most) + vp;
+      if constexpr (FULL && 16 * KS == C::PITCH) {
+        load_to_lds_at(ks, k_at, kb + i * 1024);
+        load_to_lds_at(vs, v_at, vb + i * 1024);
+      } else {                                   // features behind the head's are zeros
+        load_to_lds_at((int)kp < 2 * D ? ks + k_at : reinterpret_cast<const char *>(prompt_zeros), kb + i * 1024);
+        load_to_lds_at((int)vp < 2 * D ? vs + v_at : reinterpret_cast<const char *>(prompt_zeros), vb + i * 1024);
       }
     }
-    ahead_k += STAGE;
   };
-  // the first KC operands of the 32 keys at kb (kx: kbase)
-  constexpr int KC = KS <= 8 ? KS : 4;
-  auto read_k = [&](const unsigned char *kb, int kx, u32x4_t (&kf)[KC]) {
+  auto read_k = [&](const unsigned char *kb, u32x4_t (&kf)[KS]) __attribute__((always_inline)) {          // of the 32 keys at kb
+    int kx = kbase;
+    asm volatile("" : "+v"(kx));                 // (what is made of it is not kept through the loop)
 #pragma unroll
-    for (int ks = 0; ks < KC; ++ks) kf[ks] = *reinterpret_cast<const u32x4_t *>(kb + (kx ^ (ks * 32)));
+    for (int ks = 0; ks < KS; ++ks) kf[ks] = *reinterpret_cast<const u32x4_t *>(kb + (kx ^ (ks * 32)));
   };
 
-  issue(0); issue(1); issue(2);
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * NL) : "memory");
-  __builtin_amdgcn_s_barrier();                  // stage 0 has landed
+  for (int i = 0; i < 3; ++i) { next_slot(); issue(i); }
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");
+  __builtin_amdgcn_s_barrier();                  // slots 0 and 1 have landed
   asm volatile("" ::: "memory");
   int b = 0;
   do {
-    const PromptSeq seq = run.seq;
-    const int s = run.s, h = run.h, tile = run.tile;
-    u32x4_t qf[RT][KS];
-    int low[RT], high[RT];                       // keys that this lane's rows see
-    int all_low = -PROMPT_FAR, all_high = PROMPT_FAR;                // keys that every row of the wavefront sees
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      int token, head;
-      const bool row = prompt_row(P, seq, tile, h, (wave * RT + rt) * 32 + col, token, head);
-      const int place = seq.keys - seq.n + token;
-      low[rt] = place - P.left;
-      high[rt] = row ? place + P.right : -1;
+    const PromptSeq seq = {scalar(kept[0][wave].seq.row0), scalar(kept[0][wave].seq.n), scalar(kept[0][wave].seq.key0), scalar(kept[0][wave].seq.keys)};
+    const int h = scalar(kept[0][wave].h), tile = scalar(kept[0][wave].tile);
+    u32x4_t qf[KS];
+    int token, head;
+    const bool row = prompt_row(P, seq, tile, h, wave * 32 + col, token, head);
+    {
       const uint16_t *qp = P.q + (long long)(seq.row0 + token) * P.ldq + (long long)head * D + half * 8;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        qf[rt][ks] = u32x4_t{0u, 0u, 0u, 0u};
-        if (row && (FULL || ks * 16 + half * 8 < D)) qf[rt][ks] = *reinterpret_cast<const u32x4_t *>(qp + ks * 16);
+        qf[ks] = u32x4_t{0u, 0u, 0u, 0u};
+        if (row && (FULL || ks * 16 + half * 8 < D)) qf[ks] = *reinterpret_cast<const u32x4_t *>(qp + ks * 16);
       }
     }
-    // (rows that are none see nothing and need no mask)
-    const int w0 = wave * RT * 32 / P.tile_group, w1 = (wave * RT * 32 + RT * 32 - 1) / P.tile_group;
-    const int t_first = tile * P.tile_tokens + w0;
+    // The queries are waited for here, with what is under way to LDS: left to the compiler, which does not know of the loads in
+    // assembly, the wait stands ahead of every use in the loop below, and there it is one for all rows of K and V under way.
+    __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
+    // keys that this lane's row sees, and those that every row of the wavefront sees (rows that are none see nothing and need no mask)
+    const int place = seq.keys - seq.n + token, low = place - P.left;
+    int high = row ? place + P.right : -1;
+    high = high < seq.keys - 1 ? high : seq.keys - 1;
+    const int w0 = wave * 32 / P.tile_group, w1 = (wave * 32 + 31) / P.tile_group, t_first = tile * P.tile_tokens + w0;
     int t_last = tile * P.tile_tokens + (w1 < P.tile_tokens ? w1 : P.tile_tokens - 1);
     t_last = t_last < seq.n ? t_last : seq.n - 1;
-    const bool mine = w0 < P.tile_tokens && t_first < seq.n;         // the wavefront has rows
-    all_high = seq.keys - seq.n + t_first + P.right;
-    all_low = seq.keys - seq.n + t_last - P.left;
-    f32x16_t o[RT][NF];
-    float l[RT];                                 // of the lane's own keys: the half wave's other half has the rest
-    float ref[RT];                               // -m; NONE, fp32's largest number, where a row has seen no key yet: any score but minus infinity then makes an infinity
+    int all_high = seq.keys - seq.n + t_first + P.right;
+    const int all_low = seq.keys - seq.n + t_last - P.left;
+    all_high = all_high < seq.keys - 1 ? all_high : seq.keys - 1;
+    f32x16_t o[NF];
+    float l[2] = {0.0f, 0.0f};                   // two parts of the sum over the lane's own keys: the wave's other half has the rest
+    float ref = NONE;                            // -m; NONE, fp32's largest number, where a row has seen no key yet: any score but minus infinity then makes an infinity
     bool far_off = false;                        // some row's reference is FAR or more in size
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      ref[rt] = NONE; l[rt] = 0.0f;
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[f][i] = 0.0f;
+    // A turn of a wavefront (32 keys): the scores become probabilities while the matrix unit adds up the values of the turn before;
+    // then the scores of the next turn are formed while the values of this one are read.
+    u32x4_t kf[KS], vf[NF][2], pf[2][2];         // pf: probabilities of the turn before, of this one
+    f32x16_t x;                                  // scores
+#pragma unroll
+    for (int f = 0; f < NF; ++f) vf[f][0] = vf[f][1] = u32x4_t{0u, 0u, 0u, 0u};
+    pf[1][0] = pf[1][1] = u32x4_t{0u, 0u, 0u, 0u};
+    auto scores = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) x = mfma32<DT>(kf[ks], qf[ks], x);
+    };
+    auto add_values = [&](const u32x4_t (&p)[2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int f = 0; f < NF; ++f) o[f] = mfma32<DT>(vf[f][kk], p[kk], o[f]);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) { l[0] = add_pair<DT>(p[0][x], l[0]); l[1] = add_pair<DT>(p[1][x], l[1]); }
+    };
+    // Values that are infinite or NaN among the 32 keys from k0 on, some of which some row does not see: 0 x infinity is no number.  They
+    // are taken out of the operand, and where a row sees one, it is added to the row's output as what it is.
+    auto odd_values = [&](int k0) __attribute__((always_inline)) {
+      constexpr uint32_t INF = DT == DT_F16 ? 0x7c007c00u : 0x7f807f80u, ONE = DT == DT_F16 ? 0x3c00u : 0x3f80u;
+      uint32_t most = 0;
 #pragma unroll
       for (int f = 0; f < NF; ++f)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[rt][f][i] = 0.0f;
-    }
-    // scores of the 32 keys at kb, whose first operands are in kf
-    auto scores = [&](const unsigned char *kb, int kx, const u32x4_t (&kf)[KC], f32x16_t (&x)[RT]) {
+        for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+          for (int w = 0; w < 4; ++w) most = larger_pair(most, vf[f][kk][w] & 0x7fff7fffu);
+      if (!__any(not_finite<DT>(most))) return;
+      u32x4_t see[2];                            // ones for the keys that the lane's row sees, as the operand of probabilities
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[rt][i] = 0.0f;
+      for (int i = 0; i < 16; i += 2) {
+        const int key = k0 + 8 * (i / 4) + 4 * half + i % 4;
+        see[i / 8][(i % 8) / 2] = (key >= low && key <= high ? ONE : 0u) | (key + 1 >= low && key + 1 <= high ? ONE << 16 : 0u);
+      }
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const u32x4_t f = ks < KC ? kf[ks < KC ? ks : 0] : *reinterpret_cast<const u32x4_t *>(kb + (kx ^ (ks * 32)));
+      for (int f = 0; f < NF; ++f) {
+        asm volatile("" : "+v"(vf[f][0]), "+v"(vf[f][1]));         // (nothing of this is kept from the test above, or for the next block)
+#pragma unroll 1
+        for (int kind = 0; kind < 3; ++kind) {   // infinity, minus infinity, NaN
+          const uint32_t add = kind == 0 ? 0x7f800000u : kind == 1 ? 0xff800000u : 0x7fc00000u;
+          const uint32_t hide = kind == 2 ? 0x7fff7fffu : 0xffffffffu, other = kind == 0 ? INF : kind == 1 ? INF | 0x80008000u : 0u;
+          f32x16_t n;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) x[rt] = mfma32<DT>(f, qf[rt][ks], x[rt]);
+          for (int i = 0; i < 16; ++i) n[i] = 0.0f;
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            u32x4_t one;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {        // (arithmetic on pairs: 1 where it is one of the kind)
+              const uint32_t v = (vf[f][kk][w] & hide) ^ other;
+              one[w] = times_pair(kind == 2 ? smaller_pair(minus_pair(v, INF), 0x00010001u) : smaller_pair(v, 0x00010001u) ^ 0x00010001u, ONE * 0x00010001u);
+            }
+            n = mfma32<DT>(one, see[kk], n);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {         // (n: how many the row sees)
+            const uint32_t some = __float_as_uint(n[i]) < 1u ? __float_as_uint(n[i]) : 1u;
+            o[f][i] += __uint_as_float((0u - some) & add);
+          }
+        }
+        asm volatile("" : "+v"(vf[f][0]), "+v"(vf[f][1]));
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t odd = smaller_pair(minus_pair(vf[f][kk][w] & 0x7fff7fffu, INF - 0x00010001u), 0x00010001u);
+            vf[f][kk][w] &= ~times_pair(odd, 0xffffffffu);
+          }
       }
     };
-    const int k_first = run.keys.first + run.k_from, k_last = run.keys.first + run.k_to;
-    f32x16_t sc[RT];                             // scores of the next 32 keys
-    if (mine && k_first < k_last) {
-      u32x4_t kf[KC];
-      read_k(prompt_smem + b * 2 * BUF, kbase, kf);
-      scores(prompt_smem + b * 2 * BUF, kbase, kf, sc);
+    const int k_first = scalar(kept[0][wave].keys.first + kept[0][wave].k_from), k_last = scalar(kept[0][wave].keys.first + kept[0][wave].k_to);
+    if (k_first < k_last) {
+      read_k(prompt_smem + b * 2 * BUF, kf);
+      scores();
     }
-    for (int k0 = k_first; k0 < k_last; k0 += STAGE, b = (b + 1) & 3) {
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * NL) : "memory");      // my rows of the next stage have landed
-      __builtin_amdgcn_s_barrier();                                                  // everybody's have; the stage before has been read
-      asm volatile("" ::: "memory");
-      issue((b + 3) & 3);
-      const unsigned char *kb = prompt_smem + b * 2 * BUF, *vb = kb + BUF, *kb_next = prompt_smem + ((b + 1) & 3) * 2 * BUF;
-      if (!mine) continue;
-      const bool masked = k0 + STAGE > seq.keys || k0 + STAGE - 1 > all_high || k0 < all_low;
-      bool odd_v = false;
-      if (masked) {                              // is there a value that is infinite or NaN?
-#pragma unroll 1
-        for (int x = 0; x < BUF / 1024; ++x) {
-          const u32x4_t v = *reinterpret_cast<const u32x4_t *>(vb + x * 1024 + lane * 16);
+    bool hidden = false;                         // of the keys of the turn before, some row does not see some
+    for (int k0 = k_first; k0 < k_last; k0 += PROMPT_UNIT) {
 #pragma unroll
-          for (int w = 0; w < 4; ++w) odd_v |= not_finite<DT>(v[w]);
+      for (int c = 0; c < 2; ++c) {
+        if (c * 32 % SLOT == 0) {
+          // my rows of the next slot have landed, and what I read of the slot before has been read ...
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * NL) : "memory");
+          __builtin_amdgcn_s_barrier();          // ... and everybody's
+          asm volatile("" ::: "memory");
+          next_slot();
+          issue((b + 3) & 3);
         }
-        odd_v = __any(odd_v);
-      }
+        const unsigned char *vb = prompt_smem + b * 2 * BUF + BUF + c * 32 % SLOT * ROWB;
+        if ((c + 1) * 32 % SLOT == 0) b = (b + 1) & 3;
+        const unsigned char *kb = prompt_smem + b * 2 * BUF + (c + 1) * 32 % SLOT * ROWB;          // of the 32 keys after these
+        const int k = k0 + 32 * c;
+        const bool masked = k + 31 > all_high || k < all_low;
+        if (__builtin_expect(masked || hidden, 0)) {
+          if (hidden) odd_values(k - 32);
+          if (masked) {
+            const int up = high - k - 4 * half, down = low - k - 4 * half;
 #pragma unroll
-      for (int c = 0; c < HALVES; ++c) {         // 32 keys
-        int kx = kbase, vx = vbase, vz = vpiece ^ prompt_swizzle_v<C::PITCH>(vrow), hf = 4 * half;
-        asm volatile("" : "+v"(kx), "+v"(vx), "+v"(vz), "+v"(hf));      // (what is made of these is not kept through the loop)
-        const unsigned char *kn = c + 1 < HALVES ? kb + (c + 1) * 32 * ROWB : kb_next;      // the 32 keys after these
-        u32x4_t kf[KC];
-        read_k(kn, kx, kf);
-        auto sees = [&](int rt, int i) {         // key 8 (i / 4) + 4 half + i % 4 of the 32
-          const int at = 8 * (i / 4) + i % 4, up = high[rt] - (k0 + 32 * c) - hf, down = low[rt] - (k0 + 32 * c) - hf;
-          const int end = seq.keys - 1 - (k0 + 32 * c) - hf;
-          return at <= up && at >= down && at <= end;
-        };
-        auto hide = [&](f32x16_t (&x)[RT]) {
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (!sees(rt, i)) x[rt][i] = -__builtin_inff();
-        };
-        if (masked) hide(sc);
-        // ---- probabilities of these keys (rounded to the type: off by at most half a step, which is what the
-        // output's own rounding is off by), beside the scores of the next
-        u32x4_t pf[RT][2];
-        uint32_t any = 0;
-        auto probabilities = [&](const f32x16_t (&x)[RT]) {
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-              float p[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) p[e] = att_exp2(fmaf(x[rt][i + e], P.scale2, ref[rt]));
-              const uint32_t lo = pack2<DT>(p[0], p[1]), hi = pack2<DT>(p[2], p[3]);
-              pf[rt][i / 8][(i % 8) / 2] = lo; pf[rt][i / 8][(i % 8) / 2 + 1] = hi;
-              any = att_larger<DT>(any, lo, hi);
+            for (int i = 0; i < 16; ++i) {       // key 8 (i / 4) + 4 half + i % 4 of the 32
+              const int at = 8 * (i / 4) + i % 4;
+              if (at > up || at < down) x[i] = -__builtin_inff();
             }
-        };
-        probabilities(sc);
-        scores(kn, kx, kf, sc);
-        if (__any(att_large<DT>(any)) || far_off) {
-          f32x16_t x[RT];
-          {
-            u32x4_t kr[KC];
-            read_k(kb + c * 32 * ROWB, kx, kr);
-            scores(kb + c * 32 * ROWB, kx, kr, x);
-          }
-          if (masked) hide(x);
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            float top = x[rt][0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) top = fmaxf(top, x[rt][i]);
-            top = fmaxf(top, __shfl_xor(top, 32, 64)) * P.scale2;
-            // The fused product above has more bits than the rounded one that the reference is made of: beside a reference of 2^24 (FAR)
-            // the difference is a factor of up to 2, beside one of 2^31 an infinity or nothing.  From FAR on the wavefront rounds the
-            // products, takes the maximum of every 32 keys, and a row's largest probability is 1.
-            const bool seen = top != -__builtin_inff(), far = seen && fabsf(top) >= FAR;
-            far_off |= __any(far) != 0;
-            const float ref_new = !seen ? ref[rt] : fminf(ref[rt], far ? -top : -(top + REF));
-            const float a = att_exp2(ref_new - ref[rt]);       // (0 from NONE on)
-            ref[rt] = ref_new;
-            l[rt] *= a;
-#pragma unroll
-            for (int f = 0; f < NF; ++f)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) o[rt][f][i] *= a;
-          }
-          if (far_off) {
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-              for (int i = 0; i < 16; i += 2) {
-                float p[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                  float t = x[rt][i + e] * P.scale2;
-                  asm volatile("" : "+v"(t));    // (not fused with the sum)
-                  p[e] = att_exp2(t + ref[rt]);
-                }
-                pf[rt][i / 8][(i % 8) / 2] = pack2<DT>(p[0], p[1]);
-              }
-          } else {
-            probabilities(x);
           }
         }
+        hidden = masked;
+        u32x4_t (&p)[2] = pf[c], (&before)[2] = pf[1 - c];
+        uint32_t any = 0;
+        // probabilities, rounded to the type: off by at most half a step, which is what the output's own rounding is off by
+        auto probabilities = [&]() __attribute__((always_inline)) {
+          any = 0;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+          for (int i = 0; i < 16; i += 4) {
+            float e[4];
 #pragma unroll
-          for (int x = 0; x < 8; ++x) l[rt] = add_pair<DT>(pf[rt][x / 4][x % 4], l[rt]);
-        if (!odd_v) {
+            for (int j = 0; j < 4; ++j) e[j] = att_exp2(fmaf(x[i + j], P.scale2, ref));
+            p[i / 8][(i % 8) / 2] = pack2<DT>(e[0], e[1]); p[i / 8][(i % 8) / 2 + 1] = pack2<DT>(e[2], e[3]);
+            any = att_larger<DT>(any, p[i / 8][(i % 8) / 2], p[i / 8][(i % 8) / 2 + 1]);
+          }
+        };
+        __builtin_amdgcn_sched_barrier(0);
+        read_k(kb, kf);
+        add_values(before);
+        probabilities();
+        // Each product hides about five vector instructions of the same wavefront, an exponential counting for two.
+#pragma unroll
+        for (int i = 0; i < 2 * NF; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);       // product
+          __builtin_amdgcn_sched_group_barrier(0x100, (KS + 2 * NF - 1) / (2 * NF), 0);    // reads from LDS
+          __builtin_amdgcn_sched_group_barrier(0x400, (8 + NF - 1) / NF, 0);               // exponentials
+          __builtin_amdgcn_sched_group_barrier(0x002, (20 + NF - 1) / NF, 0);              // other vector instructions
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (__builtin_expect(__any(att_large<DT>(any)) || far_off, 0)) {
+          float top = x[0];
+#pragma unroll
+          for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+          top = fmaxf(top, __shfl_xor(top, 32, 64)) * P.scale2;
+          // The fused product above has more bits than the rounded one that the reference is made of: beside a reference of 2^24 (FAR)
+          // the difference is a factor of up to 2, beside one of 2^31 an infinity or nothing.  From FAR on the wavefront rounds the
+          // products, takes the maximum of every 32 keys, and a row's largest probability is 1.
+          const bool seen = top != -__builtin_inff(), far = seen && fabsf(top) >= FAR;
+          far_off |= __any(far) != 0;
+          const float ref_new = !seen ? ref : fminf(ref, far ? -top : -(top + REF));
+          const float a = att_exp2(ref_new - ref);               // (0 from NONE on)
+          ref = ref_new;
+          l[0] *= a; l[1] *= a;
 #pragma unroll
           for (int f = 0; f < NF; ++f)
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {     // keys 16 kk .. 16 kk + 15
-              uint2 v[2];
+            for (int i = 0; i < 16; ++i) o[f][i] *= a;
+          if (far_off) {
 #pragma unroll
-              for (int u = 0; u < 2; ++u) {      // rows 8 u + vrow: their swizzle is that of vrow with the bits of 8 u the other way
-                const int row8 = 32 * c + 16 * kk + 8 * u;
-                v[u] = read_transposed(vb + row8 * ROWB + vx + (((f * 4) ^ vz ^ prompt_swizzle_v<C::PITCH>(8 * u)) * 16));
+            for (int i = 0; i < 16; i += 2) {
+              float e[2];
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                float t = x[i + j] * P.scale2;
+                asm volatile("" : "+v"(t));      // (not fused with the sum)
+                e[j] = att_exp2(t + ref);
               }
-              const u32x4_t vf = {v[0].x, v[0].y, v[1].x, v[1].y};
-#pragma unroll
-              for (int rt = 0; rt < RT; ++rt) o[rt][f] = mfma32<DT>(vf, pf[rt][kk], o[rt][f]);
+              p[i / 8][(i % 8) / 2] = pack2<DT>(e[0], e[1]);
             }
-        } else {
-          // 0 x infinity is no number: with such a value among the keys, every row adds up the keys that it sees, one by one
-#pragma unroll 1
-          for (int kk = 0; kk < 32; ++kk) {
-            const int i0 = 4 * (kk >> 3) + (kk & 3);       // which of the lane's sixteen probabilities, of the half (kk >> 2) & 1
-            float pk[RT];
-            bool see[RT];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-              uint32_t w = 0;
-#pragma unroll
-              for (int x = 0; x < 8; ++x) w |= (i0 >> 1) == x ? pf[rt][x / 4][x % 4] : 0u;
-              pk[rt] = __shfl(i0 & 1 ? hi_f32<DT>(w) : lo_f32<DT>(w), ((kk >> 2) & 1) * 32 + col, 64);
-              const int key = k0 + 32 * c + kk;
-              see[rt] = key <= high[rt] && key >= low[rt] && key < seq.keys;
-            }
-#pragma unroll
-            for (int f = 0; f < NF; ++f)
-#pragma unroll
-              for (int g = 0; g < 4; ++g) {      // features 32 f + 8 g + 4 half .. + 3
-                int hh = half;
-                asm volatile("" : "+v"(hh));     // (an address of its own each time)
-                const int row = 32 * c + kk, piece = (4 * f + g) ^ prompt_swizzle_v<C::PITCH>(row);
-                const uint2 v = *reinterpret_cast<const uint2 *>(vb + row * ROWB + piece * 16 + hh * 8);
-                const float x[4] = {lo_f32<DT>(v.x), hi_f32<DT>(v.x), lo_f32<DT>(v.y), hi_f32<DT>(v.y)};
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-                  if (see[rt]) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[rt][f][4 * g + i] += pk[rt] * x[i];
-                  }
-              }
+          } else {
+            probabilities();
           }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        scores();
+        int vx = vbase, vz = vpiece;
+        asm volatile("" : "+v"(vx), "+v"(vz));
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {       // keys 16 kk .. 16 kk + 15; rows 8 u + vrow: their swizzle is that of vrow with the bits of 8 u the other way
+            uint2 v[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) v[u] = read_transposed(vb + (16 * kk + 8 * u) * ROWB + vx + (((f * 4) ^ vz ^ prompt_swizzle_v<C::PITCH>(8 * u)) * 16));
+            vf[f][kk] = u32x4_t{v[0].x, v[0].y, v[1].x, v[1].y};
+          }
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, (4 * NF + KS - 1) / KS, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
+    }
+    if (k_first < k_last) {
+      if (hidden) odd_values(k_first + (k_last - k_first + PROMPT_UNIT - 1) / PROMPT_UNIT * PROMPT_UNIT - 32);
+      add_values(pf[1]);
     }
 
     // ---- out: to the rows, where this workgroup had all their keys, else to the workspace
-    const bool whole = run.whole();
-    const long long which = 2LL * share + (run.first() ? 1 : 0);
-    if (mine)
+    const bool whole = scalar(kept[0][wave].whole()), first = scalar(kept[0][wave].first());
+    const long long which = 2LL * share + (first ? 1 : 0);
+    float ll = l[0] + l[1];
+    ll += __shfl_xor(ll, 32, 64);
+    if (row) {
+      if (whole) {
+        uint16_t *op = P.out + (long long)(seq.row0 + token) * P.ldo + (long long)head * D + 4 * half;
+        const float inv = ll > 0.0f || ll != ll ? 1.0f / ll : 0.0f;               // (no key seen: zeros)
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        const int r = (wave * RT + rt) * 32 + col;
-        const float ll = l[rt] + __shfl_xor(l[rt], 32, 64);
-        int token, head;
-        if (!prompt_row(P, seq, tile, h, r, token, head)) continue;
-        if (whole) {
-          uint16_t *op = P.out + (long long)(seq.row0 + token) * P.ldo + (long long)head * D + 4 * half;
-          const float inv = ll > 0.0f || ll != ll ? 1.0f / ll : 0.0f;             // (no key seen: zeros)
+        for (int f = 0; f < NF; ++f)
 #pragma unroll
-          for (int f = 0; f < NF; ++f)
+          for (int g = 0; g < 4; ++g)
+            if ((FULL && KS % 2 == 0) || 32 * f + 8 * g < D)
+              *reinterpret_cast<uint2 *>(op + 32 * f + 8 * g) =
+                  make_uint2(pack2<DT>(o[f][4 * g] * inv, o[f][4 * g + 1] * inv), pack2<DT>(o[f][4 * g + 2] * inv, o[f][4 * g + 3] * inv));
+      } else {
+        float *pp = P.part + (which * ROWS + wave * 32 + col) * C::COLS + 4 * half;
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-              if ((FULL && KS % 2 == 0) || 32 * f + 8 * g < D)
-                *reinterpret_cast<uint2 *>(op + 32 * f + 8 * g) =
-                    make_uint2(pack2<DT>(o[rt][f][4 * g] * inv, o[rt][f][4 * g + 1] * inv), pack2<DT>(o[rt][f][4 * g + 2] * inv, o[rt][f][4 * g + 3] * inv));
-        } else {
-          float *pp = P.part + (which * ROWS + r) * C::COLS + 4 * half;
+        for (int f = 0; f < NF; ++f)
 #pragma unroll
-          for (int f = 0; f < NF; ++f)
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-              *reinterpret_cast<f32x4_t *>(pp + 32 * f + 8 * g) = f32x4_t{o[rt][f][4 * g], o[rt][f][4 * g + 1], o[rt][f][4 * g + 2], o[rt][f][4 * g + 3]};
-          if (half == 0) P.part_ml[which * ROWS + r] = make_float2(ref[rt] == NONE ? -__builtin_inff() : -ref[rt], ll);
-        }
+          for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4_t *>(pp + 32 * f + 8 * g) = f32x4_t{o[f][4 * g], o[f][4 * g + 1], o[f][4 * g + 2], o[f][4 * g + 3]};
+        if (half == 0) P.part_ml[which * ROWS + wave * 32 + col] = make_float2(ref == NONE ? -__builtin_inff() : -ref, ll);
       }
-    if (!whole && run.first() && tid == 0) P.joins[share] = make_int4(s, h, tile, run.sharers());
-  } while (run.next(P));
+    }
+    if (!whole && first && tid == 0) P.joins[share] = make_int4(kept[0][wave].s, h, tile, kept[0][wave].sharers());
+  } while (advance(0));
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (rows loaded ahead and not used: their place in LDS is this workgroup's until they land)
 }
 

@@ -16,11 +16,11 @@ DEINFER_HIDDEN int launch_prompt_f16(const PromptPlan &pl, const PromptParams &P
 
 template <int DT, int KS, int WAVES, bool FULL>
 int launch_prompt_tiles(const PromptPlan &pl, const PromptParams &P, hipStream_t s) {
-  using C = PromptTile<KS, WAVES, 1>;
-  if (C::LDS > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_tile_kernel<DT, KS, WAVES, 1, FULL>),
+  using C = PromptTile<KS, WAVES>;
+  if (C::LDS > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_tile_kernel<DT, KS, WAVES, FULL>),
                                                 hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS) != hipSuccess)
     return fail(DEINFER_ERR_DEVICE, "prompt attention: LDS size refused");
-  hipLaunchKernelGGL((prompt_tile_kernel<DT, KS, WAVES, 1, FULL>), dim3((unsigned)pl.shares), dim3(C::THREADS), C::LDS, s, P);
+  hipLaunchKernelGGL((prompt_tile_kernel<DT, KS, WAVES, FULL>), dim3((unsigned)pl.shares), dim3(C::THREADS), C::LDS, s, P);
   if (int rc = check_launch("prompt attention")) return rc;
   hipLaunchKernelGGL((prompt_join_kernel<DT, C::COLS, C::ROWS>), dim3((unsigned)pl.shares, C::ROWS / 16), dim3(256), 0, s, P);
   return check_launch("prompt attention");
