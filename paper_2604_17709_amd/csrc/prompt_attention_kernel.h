@@ -643,14 +643,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) x = mfma32<DT>(kf[ks], qf[ks], x);
     };
-    auto add_values = [&](const u32x4_t (&p)[2]) __attribute__((always_inline)) {
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-        for (int f = 0; f < NF; ++f) o[f] = mfma32<DT>(vf[f][kk], p[kk], o[f]);
-#pragma unroll
-      for (int x = 0; x < 4; ++x) { l[0] = add_pair<DT>(p[0][x], l[0]); l[1] = add_pair<DT>(p[1][x], l[1]); }
-    };
     // Values that are infinite or NaN among the 32 keys from k0 on, some of which some row does not see: 0 x infinity is no number.  They
     // are taken out of the operand, and where a row sees one, it is added to the row's output as what it is.
     auto odd_values = [&](int k0) __attribute__((always_inline)) {
@@ -741,31 +733,33 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
         hidden = masked;
         u32x4_t (&p)[2] = pf[c], (&before)[2] = pf[1 - c];
         uint32_t any = 0;
-        // probabilities, rounded to the type: off by at most half a step, which is what the output's own rounding is off by
-        auto probabilities = [&]() __attribute__((always_inline)) {
-          any = 0;
-#pragma unroll
-          for (int i = 0; i < 16; i += 4) {
-            float e[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] = att_exp2(fmaf(x[i + j], P.scale2, ref));
-            p[i / 8][(i % 8) / 2] = pack2<DT>(e[0], e[1]); p[i / 8][(i % 8) / 2 + 1] = pack2<DT>(e[2], e[3]);
-            any = att_larger<DT>(any, p[i / 8][(i % 8) / 2], p[i / 8][(i % 8) / 2 + 1]);
-          }
+        // Probabilities, rounded to the type: off by at most half a step, which is what the output's own rounding is off by.  Two at a
+        // time, in three steps (the scaled score, its power, the rounding) of which each is done beside the others' next two.
+        float e[16];
+        auto scale = [&](int i) __attribute__((always_inline)) { e[i] = fmaf(x[i], P.scale2, ref); e[i + 1] = fmaf(x[i + 1], P.scale2, ref); };
+        auto power = [&](int i) __attribute__((always_inline)) { e[i] = att_exp2(e[i]); e[i + 1] = att_exp2(e[i + 1]); };
+        auto round = [&](int i) __attribute__((always_inline)) {
+          p[i / 8][(i % 8) / 2] = pack2<DT>(e[i], e[i + 1]);
+          if (i % 4 == 2) any = att_larger<DT>(any, p[i / 8][(i % 8) / 2 - 1], p[i / 8][(i % 8) / 2]);
         };
+        // ---- beside them the products that add up the values of the turn before (each hides five vector instructions, an exponential
+        // counting for two), and the reads of the next scores' operands
+        int kx = kbase, vx = vbase, vz = vpiece;
+        asm volatile("" : "+v"(kx));             // (what is made of it is not kept through the loop)
         __builtin_amdgcn_sched_barrier(0);
-        read_k(kb, kf);
-        add_values(before);
-        probabilities();
-        // Each product hides about five vector instructions of the same wavefront, an exponential counting for two.
 #pragma unroll
         for (int i = 0; i < 2 * NF; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);       // product
-          __builtin_amdgcn_sched_group_barrier(0x100, (KS + 2 * NF - 1) / (2 * NF), 0);    // reads from LDS
-          __builtin_amdgcn_sched_group_barrier(0x400, (8 + NF - 1) / NF, 0);               // exponentials
-          __builtin_amdgcn_sched_group_barrier(0x002, (20 + NF - 1) / NF, 0);              // other vector instructions
+          o[i % NF] = mfma32<DT>(vf[i % NF][i / NF], before[i / NF], o[i % NF]);
+#pragma unroll
+          for (int ks = i * KS / (2 * NF); ks < (i + 1) * KS / (2 * NF); ++ks) kf[ks] = *reinterpret_cast<const u32x4_t *>(kb + (kx ^ (ks * 32)));
+#pragma unroll
+          for (int j = i * 10 / (2 * NF); j < (i + 1) * 10 / (2 * NF); ++j) {       // ten steps
+            if (j < 8) scale(2 * j);
+            if (j >= 1 && j < 9) power(2 * j - 2);
+            if (j >= 2) round(2 * j - 4);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
         if (__builtin_expect(__any(att_large<DT>(any)) || far_off, 0)) {
           float top = x[0];
 #pragma unroll
@@ -797,34 +791,35 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
               p[i / 8][(i % 8) / 2] = pack2<DT>(e[0], e[1]);
             }
           } else {
-            probabilities();
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) { scale(i); power(i); round(i); }
           }
         }
-        __builtin_amdgcn_sched_barrier(0);
-        scores();
-        int vx = vbase, vz = vpiece;
+        // ---- the scores of the next turn; beside them the values of this turn are read, and the sum
         asm volatile("" : "+v"(vx), "+v"(vz));
-#pragma unroll
-        for (int f = 0; f < NF; ++f)
-#pragma unroll
-          for (int kk = 0; kk < 2; ++kk) {       // keys 16 kk .. 16 kk + 15; rows 8 u + vrow: their swizzle is that of vrow with the bits of 8 u the other way
-            uint2 v[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) v[u] = read_transposed(vb + (16 * kk + 8 * u) * ROWB + vx + (((f * 4) ^ vz ^ prompt_swizzle_v<C::PITCH>(8 * u)) * 16));
-            vf[f][kk] = u32x4_t{v[0].x, v[0].y, v[1].x, v[1].y};
-          }
-#pragma unroll
-        for (int i = 0; i < KS; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, (4 * NF + KS - 1) / KS, 0);
-        }
+        auto read_v = [&](int i) __attribute__((always_inline)) {  // keys 16 kk + 8 u + vrow: their swizzle is that of vrow with the bits of 8 u the other way
+          const int f = i / 4, kk = i / 2 % 2, u = i % 2;
+          const uint2 v = read_transposed(vb + (16 * kk + 8 * u) * ROWB + vx + (((f * 4) ^ vz ^ prompt_swizzle_v<C::PITCH>(8 * u)) * 16));
+          vf[f][kk][2 * u] = v.x; vf[f][kk][2 * u + 1] = v.y;
+        };
         __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          x = mfma32<DT>(kf[ks], qf[ks], x);
+#pragma unroll
+          for (int i = ks * 4 * NF / KS; i < (ks + 1) * 4 * NF / KS; ++i) read_v(i);
+#pragma unroll
+          for (int i = ks * 8 / KS; i < (ks + 1) * 8 / KS; ++i) l[i % 2] = add_pair<DT>(p[i / 4][i % 4], l[i % 2]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
     if (k_first < k_last) {
       if (hidden) odd_values(k_first + (k_last - k_first + PROMPT_UNIT - 1) / PROMPT_UNIT * PROMPT_UNIT - 32);
-      add_values(pf[1]);
+#pragma unroll
+      for (int i = 0; i < 2 * NF; ++i) o[i % NF] = mfma32<DT>(vf[i % NF][i / NF], pf[1][i / NF], o[i % NF]);
     }
 
     // ---- out: to the rows, where this workgroup had all their keys, else to the workspace
