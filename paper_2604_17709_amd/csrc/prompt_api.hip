@@ -208,7 +208,7 @@ int deinfer_prompt_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_
   P.ldq = ldq; P.ldo = ldo; P.ldk = (uint32_t)(2 * ldk); P.ldv = (uint32_t)(2 * ldv);
   P.T = (int)T; P.Tk = (int)n_keys; P.n_seqs = (int)n_seqs; P.head_dim = (int)head_dim; P.group = (int)(n_q_heads / n_kv_heads);
   P.head_tiles = (int)ceil_div(P.group, pl.rows); P.tile_group = (int)ceil_div(P.group, P.head_tiles); P.tile_tokens = pl.rows / P.tile_group;
-  P.heads = (int)n_kv_heads * P.head_tiles;
+  P.heads = (int)n_kv_heads * P.head_tiles; P.per_token = 1.0 / P.tile_tokens;
   P.left = left < 0 || left > PROMPT_FAR ? PROMPT_FAR : (int)left;
   P.right = right < 0 || right > PROMPT_FAR ? PROMPT_FAR : (int)right;
   P.scale2 = scale2;

@@ -27,6 +27,7 @@ struct PromptParams {
   uint32_t ldk, ldv;                             // in bytes
   int T, Tk, n_seqs, head_dim, group;
   int heads, head_tiles, tile_group, tile_tokens;      // key heads x parts of their query heads (head_tiles); query heads and tokens of a tile
+  double per_token;                              // 1 / tile_tokens
   int left, right;                               // at most PROMPT_FAR
   float scale2;                                  // scale log2(e): the exponentials are powers of two
   int n_shares;
@@ -58,10 +59,11 @@ __device__ __forceinline__ PromptKeys prompt_keys(const PromptParams &P, const P
   b = b < 0 ? 0 : b > q.keys ? q.keys : b;
   return {a, b - a};
 }
-// sum over i < t of a + i step, each held within [0, most]
-__device__ __forceinline__ long long clamped_series(int a, int step, int most, int t) {
-  int z = a >= 0 ? 0 : (int)(((uint32_t)(-a) + (uint32_t)step - 1) / (uint32_t)step);
-  int f = a >= most ? 0 : (int)(((uint32_t)(most - a) + (uint32_t)step - 1) / (uint32_t)step);
+// sum over i < t of a + i step, each held within [0, most]; per_step: 1 / step (x + 1/2 is at least 1 / (2 step) steps from a whole number of them,
+// and the product less than 2^-20 of that off)
+__device__ __forceinline__ long long clamped_series(int a, int step, double per_step, int most, int t) {
+  auto steps = [&](int x) { return x <= 0 ? 0 : (int)(((double)(x + step - 1) + 0.5) * per_step); };        // up to x, rounded up
+  int z = steps(-a), f = steps(most - a);
   z = z > t ? t : z; f = f > t ? t : f;
   if (f <= z) return (long long)(t - f) * most;
   return (long long)(f - z) * a + ((long long)f * (f - 1) - (long long)z * (z - 1)) / 2 * step + (long long)(t - f) * most;
@@ -69,7 +71,13 @@ __device__ __forceinline__ long long clamped_series(int a, int step, int most, i
 // work of a sequence's first t tiles of one head
 template <int START> __device__ __forceinline__ long long prompt_work(const PromptParams &P, const PromptSeq &q, int t) {
   const int c0 = q.keys - q.n, step = P.tile_tokens;
-  return (long long)t * START + clamped_series(c0 + step + P.right, step, q.keys, t) - clamped_series(c0 - P.left, step, q.keys, t);
+  return (long long)t * START + clamped_series(c0 + step + P.right, step, P.per_token, q.keys, t) - clamped_series(c0 - P.left, step, P.per_token, q.keys, t);
+}
+// a / b where the quotient is an int: a division in 64-bit floating point is off by less than one then
+__device__ __forceinline__ int small_quotient(long long a, long long b) {
+  int q = (int)((double)a / (double)b);
+  const long long r = a - q * b;
+  return r < 0 ? q - 1 : r >= b ? q + 1 : q;
 }
 __device__ __forceinline__ int prompt_tiles(const PromptParams &P, const PromptSeq &q) { return (q.n + P.tile_tokens - 1) / P.tile_tokens; }
 
@@ -120,8 +128,8 @@ template <int UNIT, int START, int THREADS> struct PromptRun {
       total += t;
     }
     total = uniform(total);
-    per_share = (total + P.n_shares - 1) / P.n_shares;
-    per_share = per_share < UNIT ? UNIT : per_share;                 // (every share between a tile's first and last then has a stage's last key)
+    per_share = (long long)((double)total / P.n_shares * (1.0 + 0x1p-50)) + 1;         // (no less than the share, whatever the roundings)
+    per_share = uniform(per_share < UNIT ? UNIT : per_share);        // (every share between a tile's first and last then has a stage's last key)
     from_work = per_share * share;
     end = from_work + per_share < total ? from_work + per_share : total;
     if (from_work >= end) return false;
@@ -142,10 +150,10 @@ template <int UNIT, int START, int THREADS> struct PromptRun {
     base = uniform(found[1]);
     seq = prompt_seq(P, s);
     const long long per_head = uniform(enter(P));
-    const long long chunk = (from_work - base) / (per_head * chunk_heads);
-    chunk_first = (int)chunk * chunk_heads;
+    const int chunk = small_quotient(from_work - base, per_head * chunk_heads);
+    chunk_first = chunk * chunk_heads;
     const int n = P.heads - chunk_first < chunk_heads ? P.heads - chunk_first : chunk_heads;
-    base += chunk * chunk_heads * per_head;
+    base += (long long)chunk * chunk_heads * per_head;
     int lo = 0, hi = (tiles - 1) / 2;            // the last pair that begins at or before from_work
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -155,7 +163,7 @@ template <int UNIT, int START, int THREADS> struct PromptRun {
     const long long ahead = pairs_work(P, per_head, pair);
     base += n * ahead;
     const long long each = pairs_work(P, per_head, pair + 1) - ahead;
-    h = (int)((from_work - base) / each);
+    h = small_quotient(from_work - base, each);
     base += h * each;
     in_chunk = n - h;
     h += chunk_first;
@@ -171,8 +179,9 @@ template <int UNIT, int START, int THREADS> struct PromptRun {
   // The sequence's tiles and chunks; its work for one head.
   __device__ __forceinline__ long long enter(const PromptParams &P) {
     tiles = prompt_tiles(P, seq);
-    const long long per_head = prompt_work<START>(P, seq, tiles), n = ((tiles + 1) / 2 * per_share + per_head / 2) / per_head;
-    chunk_heads = __builtin_amdgcn_readfirstlane((int)(n < 1 ? 1 : n > P.heads ? P.heads : n));
+    const long long per_head = prompt_work<START>(P, seq, tiles);
+    const float n = (float)((tiles + 1) / 2) * (float)per_share / (float)per_head;           // (rounded as it may be: the same in every workgroup)
+    chunk_heads = __builtin_amdgcn_readfirstlane(n < 1.5f ? 1 : n >= (float)P.heads ? P.heads : (int)(n + 0.5f));
     return per_head;
   }
   // work of the first n pairs of one head
