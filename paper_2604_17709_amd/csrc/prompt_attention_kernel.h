@@ -473,12 +473,12 @@ __global__ __launch_bounds__(ATT_THREADS) void prompt_rows_kernel(const PromptPa
 
 // ---- more rows: WAVES wavefronts with 32 rows each share the keys, SLOT at a time, through a ring of four slots in LDS.
 // KS: 16-feature steps of the first product (padded head dimension 16 KS); PITCH: features of a row in LDS.
-template <int KS_, int WAVES_, int RT_> struct PromptTile {
-  static constexpr int KS = KS_, WAVES = WAVES_, RT = RT_;
+template <int KS_, int WAVES_> struct PromptTile {
+  static constexpr int KS = KS_, WAVES = WAVES_;
   static constexpr int PITCH = KS <= 4 ? 64 : KS <= 8 ? 128 : 256;
   static constexpr int NF = (KS + 1) / 2;        // 32-feature blocks of the output
   static constexpr int SLOT = PITCH == 256 ? 32 : 64;
-  static constexpr int THREADS = 64 * WAVES, ROWS = 32 * RT * WAVES, RING = 4;
+  static constexpr int THREADS = 64 * WAVES, ROWS = 32 * WAVES, RING = 4;
   static constexpr int ROWB = 2 * PITCH, BUF = SLOT * ROWB, LDS = RING * 2 * BUF;
   static constexpr int COLS = 32 * NF;           // columns of a partial output
 };
@@ -527,9 +527,17 @@ __device__ __forceinline__ uint32_t smaller_pair(uint32_t a, uint32_t b) { retur
 __device__ __forceinline__ uint32_t times_pair(uint32_t a, uint32_t b) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(pair_t, a) * __builtin_bit_cast(pair_t, b)); }
 __device__ __forceinline__ uint32_t minus_pair(uint32_t a, uint32_t b) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(pair_t, a), __builtin_bit_cast(pair_t, b))); }
 
-template <int DT, int KS, int WAVES, int RT, bool FULL>
+// the upper half wave's a and the lower half's b change places
+__device__ __forceinline__ void halves_swap(uint32_t &a, uint32_t &b) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = r[0]; b = r[1];
+#endif
+}
+
+template <int DT, int KS, int WAVES, bool FULL>
 __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(const PromptParams P) {
-  using C = PromptTile<KS, WAVES, RT>;
+  using C = PromptTile<KS, WAVES>;
   constexpr int ROWS = C::ROWS, SLOT = C::SLOT, THREADS = C::THREADS, NF = C::NF, ROWB = C::ROWB, BUF = C::BUF, START = PROMPT_START<ROWS>;
   constexpr int CH = C::PITCH / 8;               // 16-byte pieces of a row
   constexpr int WROWS = SLOT / WAVES;            // rows of K (of V) that a wavefront loads of a slot
@@ -643,65 +651,69 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
   __builtin_amdgcn_s_barrier();                  // slots 0 and 1 have landed
   asm volatile("" ::: "memory");
   int b = 0;
-  do {
-    const PromptSeq seq = {scalar(kept[0][wave].seq.row0), scalar(kept[0][wave].seq.n), scalar(kept[0][wave].seq.key0), scalar(kept[0][wave].seq.keys)};
-    const int h = scalar(kept[0][wave].h), tile = scalar(kept[0][wave].tile);
-    u32x4_t qf[RT][KS];
-    int low[RT], high[RT];                       // keys that this lane's rows see
+  // The present tile: the lane's row (its token and head of the tile are always the same), its queries and the keys that it sees.
+  const int row_token = (wave * 32 + col) / P.tile_group, row_head = (wave * 32 + col) % P.tile_group;
+  PromptSeq seq;
+  int h, tile, low, high, k_first, k_last;
+  bool row;
+  long long row_at, head_at;                     // the row's token, and its head's first feature
+  u32x4_t qf[KS];
+  auto open_tile = [&]() __attribute__((always_inline)) {
+    const Run &at = kept[0][wave];
+    seq = {scalar(at.seq.row0), scalar(at.seq.n), scalar(at.seq.key0), scalar(at.seq.keys)};
+    h = scalar(at.h); tile = scalar(at.tile);
+    k_first = scalar(at.keys.first + at.k_from); k_last = scalar(at.keys.first + at.k_to);
+    const int kv = h / P.head_tiles, g0 = (h - kv * P.head_tiles) * P.tile_group, token = tile * P.tile_tokens + row_token;
+    row = row_token < P.tile_tokens && token < seq.n && g0 + row_head < P.group;
+    row_at = seq.row0 + token;
+    head_at = (long long)(kv * P.group + g0 + row_head) * D;
+    const uint16_t *qp = P.q + row_at * P.ldq + head_at + half * 8;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      int token, head;
-      const bool row = prompt_row(P, seq, tile, h, (wave * RT + rt) * 32 + col, token, head);
-      const uint16_t *qp = P.q + (long long)(seq.row0 + token) * P.ldq + (long long)head * D + half * 8;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        qf[rt][ks] = u32x4_t{0u, 0u, 0u, 0u};
-        if (row && (FULL || ks * 16 + half * 8 < D)) qf[rt][ks] = *reinterpret_cast<const u32x4_t *>(qp + ks * 16);
-      }
-      const int place = seq.keys - seq.n + token;
-      low[rt] = place - P.left;
-      high[rt] = row ? place + P.right : -1;
-      high[rt] = high[rt] < seq.keys - 1 ? high[rt] : seq.keys - 1;
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[ks] = u32x4_t{0u, 0u, 0u, 0u};
+      if (row && (FULL || ks * 16 + half * 8 < D)) qf[ks] = *reinterpret_cast<const u32x4_t *>(qp + ks * 16);
     }
+    const int place = seq.keys - seq.n + token;
+    low = place - P.left;
+    high = row ? place + P.right : -1;
+    high = high < seq.keys - 1 ? high : seq.keys - 1;
+  };
+  open_tile();
+  bool more;
+  do {
     // The queries are waited for here, with what is under way to LDS: left to the compiler, which does not know of the loads in
     // assembly, the wait stands ahead of every use in the loop below, and there it is one for all rows of K and V under way.
     __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
     // keys that every row of the wavefront sees (rows that are none see nothing and need no mask)
-    const int w0 = wave * RT * 32 / P.tile_group, w1 = (wave * RT * 32 + RT * 32 - 1) / P.tile_group, t_first = tile * P.tile_tokens + w0;
+    const int w0 = wave * 32 / P.tile_group, w1 = (wave * 32 + 31) / P.tile_group, t_first = tile * P.tile_tokens + w0;
     int t_last = tile * P.tile_tokens + (w1 < P.tile_tokens ? w1 : P.tile_tokens - 1);
     t_last = t_last < seq.n ? t_last : seq.n - 1;
     int all_high = seq.keys - seq.n + t_first + P.right;
     const int all_low = seq.keys - seq.n + t_last - P.left;
     all_high = all_high < seq.keys - 1 ? all_high : seq.keys - 1;
-    f32x16_t o[RT][NF];
-    float l[RT][2];                              // two parts of the sum over the lane's own keys: the wave's other half has the rest
-    float ref[RT];                               // -m; NONE, fp32's largest number, where a row has seen no key yet: any score but minus infinity then makes an infinity
+    f32x16_t o[NF];
+    float l[2];                                  // two parts of the sum over the lane's own keys: the wave's other half has the rest
+    float ref;                                   // -m; NONE, fp32's largest number, where a row has seen no key yet: any score but minus infinity then makes an infinity
     bool far_off = false;                        // some row's reference is FAR or more in size
     // A turn of a wavefront (32 keys): the scores become probabilities while the matrix unit adds up the values of the turn before;
     // then the scores of the next turn are formed while the values of this one are read.
-    u32x4_t kf[KS], vf[NF][2], pf[2][RT][2];     // pf: probabilities of the turn before, of this one
-    f32x16_t x[RT];                              // scores
+    u32x4_t kf[KS], vf[NF][2], pf[2][2];         // pf: probabilities of the turn before, of this one
+    f32x16_t x;                                  // scores
+    l[0] = l[1] = 0.0f;
+    ref = NONE;
+    pf[1][0] = pf[1][1] = u32x4_t{0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      l[rt][0] = l[rt][1] = 0.0f;
-      ref[rt] = NONE;
-      pf[1][rt][0] = pf[1][rt][1] = u32x4_t{0u, 0u, 0u, 0u};
+    for (int f = 0; f < NF; ++f)
 #pragma unroll
-      for (int f = 0; f < NF; ++f)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[rt][f][i] = 0.0f;
-    }
+      for (int i = 0; i < 16; ++i) o[f][i] = 0.0f;
 #pragma unroll
     for (int f = 0; f < NF; ++f) vf[f][0] = vf[f][1] = u32x4_t{0u, 0u, 0u, 0u};
     auto scores = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[rt][i] = 0.0f;
+      for (int i = 0; i < 16; ++i) x[i] = 0.0f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) x[rt] = mfma32<DT>(kf[ks], qf[rt][ks], x[rt]);
+        x = mfma32<DT>(kf[ks], qf[ks], x);
     };
     // Values that are infinite or NaN among the 32 keys from k0 on, some of which some row does not see: 0 x infinity is no number.  They
     // are taken out of the operand, and where a row sees one, it is added to the row's output as what it is.
@@ -715,14 +727,12 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
 #pragma unroll
           for (int w = 0; w < 4; ++w) most = larger_pair(most, vf[f][kk][w] & 0x7fff7fffu);
       if (!__any(not_finite<DT>(most))) return;
-      u32x4_t see[RT][2];                        // ones for the keys that the lane's rows see, as the operand of probabilities
+      u32x4_t see[2];                            // ones for the keys that the lane's rows see, as the operand of probabilities
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          const int key = k0 + 8 * (i / 4) + 4 * half + i % 4;
-          see[rt][i / 8][(i % 8) / 2] = (key >= low[rt] && key <= high[rt] ? ONE : 0u) | (key + 1 >= low[rt] && key + 1 <= high[rt] ? ONE << 16 : 0u);
-        }
+      for (int i = 0; i < 16; i += 2) {
+        const int key = k0 + 8 * (i / 4) + 4 * half + i % 4;
+        see[i / 8][(i % 8) / 2] = (key >= low && key <= high ? ONE : 0u) | (key + 1 >= low && key + 1 <= high ? ONE << 16 : 0u);
+      }
 #pragma unroll
       for (int f = 0; f < NF; ++f) {
         asm volatile("" : "+v"(vf[f][0]), "+v"(vf[f][1]));         // (nothing of this is kept from the test above, or for the next block)
@@ -730,11 +740,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
         for (int kind = 0; kind < 3; ++kind) {   // infinity, minus infinity, NaN
           const uint32_t add = kind == 0 ? 0x7f800000u : kind == 1 ? 0xff800000u : 0x7fc00000u;
           const uint32_t hide = kind == 2 ? 0x7fff7fffu : 0xffffffffu, other = kind == 0 ? INF : kind == 1 ? INF | 0x80008000u : 0u;
-          f32x16_t n[RT];
+          f32x16_t n;
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) n[rt][i] = 0.0f;
+          for (int i = 0; i < 16; ++i) n[i] = 0.0f;
 #pragma unroll
           for (int kk = 0; kk < 2; ++kk) {
             u32x4_t one;
@@ -743,16 +751,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
               const uint32_t v = (vf[f][kk][w] & hide) ^ other;
               one[w] = times_pair(kind == 2 ? smaller_pair(minus_pair(v, INF), 0x00010001u) : smaller_pair(v, 0x00010001u) ^ 0x00010001u, ONE * 0x00010001u);
             }
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) n[rt] = mfma32<DT>(one, see[rt][kk], n[rt]);
+            n = mfma32<DT>(one, see[kk], n);
           }
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {       // (n: how many the row sees)
-              const uint32_t some = __float_as_uint(n[rt][i]) < 1u ? __float_as_uint(n[rt][i]) : 1u;
-              o[rt][f][i] += __uint_as_float((0u - some) & add);
-            }
+          for (int i = 0; i < 16; ++i) {       // (n: how many the row sees)
+            const uint32_t some = __float_as_uint(n[i]) < 1u ? __float_as_uint(n[i]) : 1u;
+            o[f][i] += __uint_as_float((0u - some) & add);
+          }
         }
         asm volatile("" : "+v"(vf[f][0]), "+v"(vf[f][1]));
 #pragma unroll
@@ -764,7 +769,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
           }
       }
     };
-    const int k_first = scalar(kept[0][wave].keys.first + kept[0][wave].k_from), k_last = scalar(kept[0][wave].keys.first + kept[0][wave].k_to);
     if (k_first < k_last) {
       read_k(prompt_smem + b * 2 * BUF, kf);
       scores();
@@ -789,87 +793,77 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
         if (__builtin_expect(masked || hidden, 0)) {
           if (hidden) odd_values(k - 32);
           if (masked) {
+            const int up = high - k - 4 * half, down = low - k - 4 * half;
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-              const int up = high[rt] - k - 4 * half, down = low[rt] - k - 4 * half;
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {     // key 8 (i / 4) + 4 half + i % 4 of the 32
-                const int at = 8 * (i / 4) + i % 4;
-                if (at > up || at < down) x[rt][i] = -__builtin_inff();
-              }
+            for (int i = 0; i < 16; ++i) {     // key 8 (i / 4) + 4 half + i % 4 of the 32
+              const int at = 8 * (i / 4) + i % 4;
+              if (at > up || at < down) x[i] = -__builtin_inff();
             }
           }
         }
         hidden = masked;
-        u32x4_t (&p)[RT][2] = pf[c], (&before)[RT][2] = pf[1 - c];
+        u32x4_t (&p)[2] = pf[c], (&before)[2] = pf[1 - c];
         uint32_t any = 0;
         // Probabilities, rounded to the type: off by at most half a step, which is what the output's own rounding is off by.  Two at a
         // time, in three steps (the scaled score, its power, the rounding) of which each is done beside the others' next two.
-        float e[RT][16];
-        auto scale = [&](int at) __attribute__((always_inline)) { const int r = at / 16, i = at % 16; e[r][i] = fmaf(x[r][i], P.scale2, ref[r]); e[r][i + 1] = fmaf(x[r][i + 1], P.scale2, ref[r]); };
-        auto power = [&](int at) __attribute__((always_inline)) { const int r = at / 16, i = at % 16; e[r][i] = att_exp2(e[r][i]); e[r][i + 1] = att_exp2(e[r][i + 1]); };
-        auto round = [&](int at) __attribute__((always_inline)) {
-          const int r = at / 16, i = at % 16;
-          p[r][i / 8][(i % 8) / 2] = pack2<DT>(e[r][i], e[r][i + 1]);
-          if (i % 4 == 2) any = att_larger<DT>(any, p[r][i / 8][(i % 8) / 2 - 1], p[r][i / 8][(i % 8) / 2]);
+        float e[16];
+        auto scale = [&](int i) __attribute__((always_inline)) { e[i] = fmaf(x[i], P.scale2, ref); e[i + 1] = fmaf(x[i + 1], P.scale2, ref); };
+        auto power = [&](int i) __attribute__((always_inline)) { e[i] = att_exp2(e[i]); e[i + 1] = att_exp2(e[i + 1]); };
+        auto round = [&](int i) __attribute__((always_inline)) {
+          p[i / 8][(i % 8) / 2] = pack2<DT>(e[i], e[i + 1]);
+          if (i % 4 == 2) any = att_larger<DT>(any, p[i / 8][(i % 8) / 2 - 1], p[i / 8][(i % 8) / 2]);
         };
         // ---- beside them the products that add up the values of the turn before (each hides five vector instructions, an exponential
         // counting for two), and the reads of the next scores' operands
         int kx = kbase, vx = vbase, vz = vpiece;
         asm volatile("" : "+v"(kx));             // (what is made of it is not kept through the loop)
         __builtin_amdgcn_sched_barrier(0);
-        constexpr int N1 = 2 * NF * RT, STEPS = 8 * RT + 2, N2 = KS * RT, N3 = (2 * N2 + 2) / 3;      // (the values' last reads have a third of the products to come back)
+        constexpr int N1 = 2 * NF, STEPS = 10, N3 = (2 * KS + 2) / 3;    // (the values' last reads have a third of the products to come back)
 #pragma unroll
         for (int i = 0; i < N1; ++i) {
-          const int rt = i % RT, f = i / RT % NF, kk = i / RT / NF;
-          o[rt][f] = mfma32<DT>(vf[f][kk], before[rt][kk], o[rt][f]);
+          o[i % NF] = mfma32<DT>(vf[i % NF][i / NF], before[i / NF], o[i % NF]);
 #pragma unroll
           for (int ks = i * KS / N1; ks < (i + 1) * KS / N1; ++ks) kf[ks] = *reinterpret_cast<const u32x4_t *>(kb + (kx ^ (ks * 32)));
 #pragma unroll
           for (int j = i * STEPS / N1; j < (i + 1) * STEPS / N1; ++j) {
-            if (j < 8 * RT) scale(2 * j);
-            if (j >= 1 && j <= 8 * RT) power(2 * j - 2);
+            if (j < 8) scale(2 * j);
+            if (j >= 1 && j <= 8) power(2 * j - 2);
             if (j >= 2) round(2 * j - 4);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
         if (__builtin_expect(__any(att_large<DT>(any)) || far_off, 0)) {
+          float top = x[0];
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            float top = x[rt][0];
+          for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+          top = fmaxf(top, __shfl_xor(top, 32, 64)) * P.scale2;
+          // The fused product above has more bits than the rounded one that the reference is made of: beside a reference of 2^24 (FAR)
+          // the difference is a factor of up to 2, beside one of 2^31 an infinity or nothing.  From FAR on the wavefront rounds the
+          // products, takes the maximum of every 32 keys, and a row's largest probability is 1.
+          const bool seen = top != -__builtin_inff(), far = seen && fabsf(top) >= FAR;
+          far_off |= __any(far) != 0;
+          const float ref_new = !seen ? ref : fminf(ref, far ? -top : -(top + REF));
+          const float a = att_exp2(ref_new - ref);         // (0 from NONE on)
+          ref = ref_new;
+          l[0] *= a; l[1] *= a;
 #pragma unroll
-            for (int i = 1; i < 16; ++i) top = fmaxf(top, x[rt][i]);
-            top = fmaxf(top, __shfl_xor(top, 32, 64)) * P.scale2;
-            // The fused product above has more bits than the rounded one that the reference is made of: beside a reference of 2^24 (FAR)
-            // the difference is a factor of up to 2, beside one of 2^31 an infinity or nothing.  From FAR on the wavefront rounds the
-            // products, takes the maximum of every 32 keys, and a row's largest probability is 1.
-            const bool seen = top != -__builtin_inff(), far = seen && fabsf(top) >= FAR;
-            far_off |= __any(far) != 0;
-            const float ref_new = !seen ? ref[rt] : fminf(ref[rt], far ? -top : -(top + REF));
-            const float a = att_exp2(ref_new - ref[rt]);         // (0 from NONE on)
-            ref[rt] = ref_new;
-            l[rt][0] *= a; l[rt][1] *= a;
+          for (int f = 0; f < NF; ++f)
 #pragma unroll
-            for (int f = 0; f < NF; ++f)
+            for (int i = 0; i < 16; ++i) o[f][i] *= a;
 #pragma unroll
-              for (int i = 0; i < 16; ++i) o[rt][f][i] *= a;
-          }
+          for (int i = 0; i < 16; i += 2) {
+            if (far_off) {
+              float t[2];
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-              if (far_off) {
-                float t[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                  t[j] = x[rt][i + j] * P.scale2;
-                  asm volatile("" : "+v"(t[j])); // (not fused with the sum)
-                }
-                p[rt][i / 8][(i % 8) / 2] = pack2<DT>(att_exp2(t[0] + ref[rt]), att_exp2(t[1] + ref[rt]));
-              } else {
-                scale(16 * rt + i); power(16 * rt + i); round(16 * rt + i);
+              for (int j = 0; j < 2; ++j) {
+                t[j] = x[i + j] * P.scale2;
+                asm volatile("" : "+v"(t[j])); // (not fused with the sum)
               }
+              p[i / 8][(i % 8) / 2] = pack2<DT>(att_exp2(t[0] + ref), att_exp2(t[1] + ref));
+            } else {
+              scale(i); power(i); round(i);
             }
+          }
         }
         // ---- the scores of the next turn; beside them the values of this turn are read, and the sum
         asm volatile("" : "+v"(vx), "+v"(vz));
@@ -880,64 +874,60 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
         };
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+        for (int i = 0; i < 16; ++i) x[i] = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) x[rt][i] = 0.0f;
-#pragma unroll
-        for (int n = 0; n < N2; ++n) {
-          const int rt = n % RT, ks = n / RT;
-          x[rt] = mfma32<DT>(kf[ks], qf[rt][ks], x[rt]);
+        for (int n = 0; n < KS; ++n) {
+          x = mfma32<DT>(kf[n], qf[n], x);
 #pragma unroll
           for (int i = n * 4 * NF / N3; i < (n + 1) * 4 * NF / N3 && i < 4 * NF; ++i) read_v(i);
           // (rows to come are asked for in the turn that begins a slot)
-          if (c * 32 % SLOT == 0) issue(place, n * 2 * NL / N2, (n + 1) * 2 * NL / N2);
+          if (c * 32 % SLOT == 0) issue(place, n * 2 * NL / KS, (n + 1) * 2 * NL / KS);
 #pragma unroll
-          for (int i = n * 8 * RT / N2; i < (n + 1) * 8 * RT / N2; ++i) l[i / 8][i % 2] = add_pair<DT>(p[i / 8][i / 4 % 2][i % 4], l[i / 8][i % 2]);
+          for (int i = n * 8 / KS; i < (n + 1) * 8 / KS; ++i) l[i % 2] = add_pair<DT>(p[i / 4][i % 4], l[i % 2]);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
-    if (k_first < k_last) {
-      if (hidden) odd_values(k_first + (k_last - k_first + PROMPT_UNIT - 1) / PROMPT_UNIT * PROMPT_UNIT - 32);
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-        for (int f = 0; f < NF; ++f)
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) o[rt][f] = mfma32<DT>(vf[f][kk], pf[1][rt][kk], o[rt][f]);
-    }
+    if (k_first < k_last && hidden) odd_values(k_first + (k_last - k_first + PROMPT_UNIT - 1) / PROMPT_UNIT * PROMPT_UNIT - 32);
 
-    // ---- out: to the rows, where this workgroup had all their keys, else to the workspace
-    const bool whole = scalar(kept[0][wave].whole()), first = scalar(kept[0][wave].first());
-    const long long which = 2LL * share + (first ? 1 : 0);
+    // ---- out: to the rows, where this workgroup had all their keys, else to the workspace; the next tile's queries are asked for
+    // ahead of that
+    const Run &at = kept[0][wave];
+    const bool whole = scalar(at.whole()), first = scalar(at.first()), to_row = row, any_keys = k_first < k_last;
+    if (!whole && first && tid == 0) P.joins[share] = make_int4(at.s, h, tile, at.sharers());
+    uint16_t *op = P.out + row_at * P.ldo + head_at + 8 * half;
+    const long long part_at = (2LL * share + (first ? 1 : 0)) * ROWS + wave * 32 + col;
+    more = advance(0);
+    if (more) open_tile();
+    if (any_keys)
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int r = (wave * RT + rt) * 32 + col;
-      float ll = l[rt][0] + l[rt][1];
-      ll += __shfl_xor(ll, 32, 64);
-      int token, head;
-      if (!prompt_row(P, seq, tile, h, r, token, head)) continue;
-      if (whole) {
-        uint16_t *op = P.out + (long long)(seq.row0 + token) * P.ldo + (long long)head * D + 4 * half;
-        const float inv = ll > 0.0f || ll != ll ? 1.0f / ll : 0.0f;               // (no key seen: zeros)
+      for (int i = 0; i < 2 * NF; ++i) o[i % NF] = mfma32<DT>(vf[i % NF][i / NF], pf[1][i / NF], o[i % NF]);
+    float ll = l[0] + l[1];
+    ll += __shfl_xor(ll, 32, 64);
+    if (whole) {
+      const float inv = ll > 0.0f || ll != ll ? 1.0f / ll : 0.0f;                 // (no key seen: zeros)
 #pragma unroll
-        for (int f = 0; f < NF; ++f)
+      for (int f = 0; f < NF; ++f)
 #pragma unroll
-          for (int g = 0; g < 4; ++g)
-            if ((FULL && KS % 2 == 0) || 32 * f + 8 * g < D)
-              *reinterpret_cast<uint2 *>(op + 32 * f + 8 * g) =
-                  make_uint2(pack2<DT>(o[rt][f][4 * g] * inv, o[rt][f][4 * g + 1] * inv), pack2<DT>(o[rt][f][4 * g + 2] * inv, o[rt][f][4 * g + 3] * inv));
-      } else {
-        float *pp = P.part + (which * ROWS + r) * C::COLS + 4 * half;
+        for (int g = 0; g < 4; g += 2) {         // features 8 g .. 8 g + 15 of the block: the wave's halves have four of each eight, and change them for all of one eight
+          uint32_t w[2][2];
 #pragma unroll
-        for (int f = 0; f < NF; ++f)
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4_t *>(pp + 32 * f + 8 * g) = f32x4_t{o[rt][f][4 * g], o[rt][f][4 * g + 1], o[rt][f][4 * g + 2], o[rt][f][4 * g + 3]};
-        if (half == 0) P.part_ml[which * ROWS + r] = make_float2(ref[rt] == NONE ? -__builtin_inff() : -ref[rt], ll);
-      }
+            for (int j = 0; j < 2; ++j) w[i][j] = pack2<DT>(o[f][4 * (g + i) + 2 * j] * inv, o[f][4 * (g + i) + 2 * j + 1] * inv);
+          halves_swap(w[0][0], w[1][0]); halves_swap(w[0][1], w[1][1]);
+          if (to_row && ((FULL && KS % 2 == 0) || 32 * f + 8 * (g + half) < D))
+            *reinterpret_cast<u32x4_t *>(op + 32 * f + 8 * g) = u32x4_t{w[0][0], w[0][1], w[1][0], w[1][1]};
+        }
+    } else if (to_row) {
+      float *pp = P.part + part_at * C::COLS + 4 * half;
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4_t *>(pp + 32 * f + 8 * g) = f32x4_t{o[f][4 * g], o[f][4 * g + 1], o[f][4 * g + 2], o[f][4 * g + 3]};
+      if (half == 0) P.part_ml[part_at] = make_float2(ref == NONE ? -__builtin_inff() : -ref, ll);
     }
-    if (!whole && first && tid == 0) P.joins[share] = make_int4(kept[0][wave].s, h, tile, kept[0][wave].sharers());
-  } while (advance(0));
+  } while (more);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (rows loaded ahead and not used: their place in LDS is this workgroup's until they land)
 }
 

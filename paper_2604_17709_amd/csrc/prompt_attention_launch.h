@@ -14,13 +14,13 @@ struct PromptPlan {
 DEINFER_HIDDEN int launch_prompt_bf16(const PromptPlan &pl, const PromptParams &P, hipStream_t s);
 DEINFER_HIDDEN int launch_prompt_f16(const PromptPlan &pl, const PromptParams &P, hipStream_t s);
 
-template <int DT, int KS, int WAVES, int RT, bool FULL>
+template <int DT, int KS, int WAVES, bool FULL>
 int launch_prompt_tiles(const PromptPlan &pl, const PromptParams &P, hipStream_t s) {
-  using C = PromptTile<KS, WAVES, RT>;
-  if (C::LDS > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_tile_kernel<DT, KS, WAVES, RT, FULL>),
+  using C = PromptTile<KS, WAVES>;
+  if (C::LDS > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_tile_kernel<DT, KS, WAVES, FULL>),
                                                 hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS) != hipSuccess)
     return fail(DEINFER_ERR_DEVICE, "prompt attention: LDS size refused");
-  hipLaunchKernelGGL((prompt_tile_kernel<DT, KS, WAVES, RT, FULL>), dim3((unsigned)pl.shares), dim3(C::THREADS), C::LDS, s, P);
+  hipLaunchKernelGGL((prompt_tile_kernel<DT, KS, WAVES, FULL>), dim3((unsigned)pl.shares), dim3(C::THREADS), C::LDS, s, P);
   if (int rc = check_launch("prompt attention")) return rc;
   hipLaunchKernelGGL((prompt_join_kernel<DT, C::COLS, C::ROWS>), dim3((unsigned)pl.shares, C::ROWS / 16), dim3(256), 0, s, P);
   return check_launch("prompt attention");
@@ -28,10 +28,9 @@ int launch_prompt_tiles(const PromptPlan &pl, const PromptParams &P, hipStream_t
 template <int DT, int KS>
 int launch_prompt_steps(const PromptPlan &pl, const PromptParams &P, hipStream_t s) {
   const bool full = P.head_dim == 16 * KS;
-  constexpr int W256 = 8, R256 = 1;
   if constexpr (KS <= 8)
-    if (pl.rows == 256) return full ? launch_prompt_tiles<DT, KS, W256, R256, true>(pl, P, s) : launch_prompt_tiles<DT, KS, W256, R256, false>(pl, P, s);
-  return full ? launch_prompt_tiles<DT, KS, 4, 1, true>(pl, P, s) : launch_prompt_tiles<DT, KS, 4, 1, false>(pl, P, s);
+    if (pl.rows == 256) return full ? launch_prompt_tiles<DT, KS, 8, true>(pl, P, s) : launch_prompt_tiles<DT, KS, 8, false>(pl, P, s);
+  return full ? launch_prompt_tiles<DT, KS, 4, true>(pl, P, s) : launch_prompt_tiles<DT, KS, 4, false>(pl, P, s);
 }
 template <int DT, int DP>
 int launch_prompt_rows(const PromptPlan &pl, const PromptParams &P, hipStream_t s) {
