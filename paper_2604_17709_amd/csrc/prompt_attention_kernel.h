@@ -542,6 +542,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
   constexpr int CH = C::PITCH / 8;               // 16-byte pieces of a row
   constexpr int WROWS = SLOT / WAVES;            // rows of K (of V) that a wavefront loads of a slot
   constexpr int RPI = 64 / CH, NL = WROWS / RPI; // rows of one load instruction, load instructions
+  constexpr bool LEAVE = SLOT == 64;             // turns in which the wavefront's rows see nothing are left to the others (heads of 256 have no registers for it)
   constexpr float REF = DT == DT_F16 ? -12.0f : 16.0f, NONE = 3.402823466e38f, FAR = 16777216.0f;
   static_assert(NL * RPI == WROWS, "whole load instructions");
   extern __shared__ __attribute__((aligned(16))) unsigned char prompt_smem[];   // [RING][K, V][SLOT][ROWB]
@@ -691,6 +692,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
     int all_high = seq.keys - seq.n + t_first + P.right;
     const int all_low = seq.keys - seq.n + t_last - P.left;
     all_high = all_high < seq.keys - 1 ? all_high : seq.keys - 1;
+    // Keys that some row of it sees are in [some_low, some_high] (none: it has no rows).  Turns beyond are left out but for one on
+    // either side, in which nothing is seen: the last adds up the values of the turn before.
+    const int some_low = seq.keys - seq.n + t_first - P.left, some_high = w0 < P.tile_tokens && t_first < seq.n ? seq.keys - seq.n + t_last + P.right : -PROMPT_FAR;
     f32x16_t o[NF];
     float l[2];                                  // two parts of the sum over the lane's own keys: the wave's other half has the rest
     float ref;                                   // -m; NONE, fp32's largest number, where a row has seen no key yet: any score but minus infinity then makes an infinity
@@ -701,7 +705,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
     f32x16_t x;                                  // scores
     l[0] = l[1] = 0.0f;
     ref = NONE;
-    pf[1][0] = pf[1][1] = u32x4_t{0u, 0u, 0u, 0u};
+    pf[0][0] = pf[0][1] = pf[1][0] = pf[1][1] = u32x4_t{0u, 0u, 0u, 0u};
 #pragma unroll
     for (int f = 0; f < NF; ++f)
 #pragma unroll
@@ -783,12 +787,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
           __builtin_amdgcn_s_barrier();          // ... and everybody's
           asm volatile("" ::: "memory");
           next_slot();
+          issue((b + 3) & 3, 0, 2 * NL);
         }
-        const int place = (b + 3) & 3;           // of the ring, for what is loaded in this turn
         const unsigned char *vb = prompt_smem + b * 2 * BUF + BUF + c * 32 % SLOT * ROWB;
         if ((c + 1) * 32 % SLOT == 0) b = (b + 1) & 3;
         const unsigned char *kb = prompt_smem + b * 2 * BUF + (c + 1) * 32 % SLOT * ROWB;          // of the 32 keys after these
         const int k = k0 + 32 * c;
+        if (LEAVE && (k > some_high + 32 || k + 63 < some_low)) continue;
         const bool masked = k + 31 > all_high || k < all_low;
         if (__builtin_expect(masked || hidden, 0)) {
           if (hidden) odd_values(k - 32);
@@ -880,26 +885,26 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
           x = mfma32<DT>(kf[n], qf[n], x);
 #pragma unroll
           for (int i = n * 4 * NF / N3; i < (n + 1) * 4 * NF / N3 && i < 4 * NF; ++i) read_v(i);
-          // (rows to come are asked for in the turn that begins a slot)
-          if (c * 32 % SLOT == 0) issue(place, n * 2 * NL / KS, (n + 1) * 2 * NL / KS);
 #pragma unroll
           for (int i = n * 8 / KS; i < (n + 1) * 8 / KS; ++i) l[i % 2] = add_pair<DT>(p[i / 4][i % 4], l[i % 2]);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
-    if (k_first < k_last && hidden) odd_values(k_first + (k_last - k_first + PROMPT_UNIT - 1) / PROMPT_UNIT * PROMPT_UNIT - 32);
+    const int k_end = k_first + (k_last - k_first + PROMPT_UNIT - 1) / PROMPT_UNIT * PROMPT_UNIT - 32;        // of the last turn
+    const bool rest = k_first < k_last && (!LEAVE || k_end <= some_high);        // the last turn's values are to be added
+    if (rest && hidden) odd_values(k_end);
 
     // ---- out: to the rows, where this workgroup had all their keys, else to the workspace; the next tile's queries are asked for
     // ahead of that
     const Run &at = kept[0][wave];
-    const bool whole = scalar(at.whole()), first = scalar(at.first()), to_row = row, any_keys = k_first < k_last;
+    const bool whole = scalar(at.whole()), first = scalar(at.first()), to_row = row;
     if (!whole && first && tid == 0) P.joins[share] = make_int4(at.s, h, tile, at.sharers());
     uint16_t *op = P.out + row_at * P.ldo + head_at + 8 * half;
     const long long part_at = (2LL * share + (first ? 1 : 0)) * ROWS + wave * 32 + col;
     more = advance(0);
     if (more) open_tile();
-    if (any_keys)
+    if (rest)
 #pragma unroll
       for (int i = 0; i < 2 * NF; ++i) o[i % NF] = mfma32<DT>(vf[i % NF][i / NF], pf[1][i / NF], o[i % NF]);
     float ll = l[0] + l[1];
