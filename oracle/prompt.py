@@ -77,16 +77,11 @@ def attention(q, k, v, q_start, k_start, n_q, n_kv, left, right, scale, out):
         for h in range(n_q):
             of = slice(h // group * D, (h // group + 1) * D)
             at = slice(h * D, (h + 1) * D)
-            for i in range(rows):
-                see = np.nonzero(sees[i])[0]
-                if len(see) == 0:
-                    out[r0 + i, at] = 0.0
-                    continue
-                x = scale * (k[j0 + see, of] @ q[r0 + i, at])
-                top = np.max(x)
-                if top == -math.inf:
-                    out[r0 + i, at] = 0.0
-                    continue
-                p = np.exp(x - top)
-                out[r0 + i, at] = (p / np.sum(p)) @ v[j0 + see, of]
+            if rows == 0:
+                continue
+            x = np.where(sees, scale * (q[r0:r0 + rows, at] @ k[j0:j0 + keys, of].T), -math.inf) if keys else np.full((rows, 1), -math.inf)
+            top = np.max(x, axis=1, keepdims=True)
+            p = np.exp(x - np.where(top == -math.inf, 0.0, top))
+            total = np.sum(p, axis=1, keepdims=True)
+            out[r0:r0 + rows, at] = (p / np.where(total > 0.0, total, 1.0)) @ v[j0:j0 + keys, of] if keys else 0.0
     return out

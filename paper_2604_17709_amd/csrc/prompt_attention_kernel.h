@@ -585,7 +585,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
     steady = 0;
     if (over) return;
     if (after < 0) after = scalar(kept[1][wave].k_from);
-    while (after >= scalar(kept[1][wave].k_to)) {                  // (tiles without keys have no slots)
+    // (a tile's slots are those of whole units; one without keys has none)
+    auto units_end = [&] { return (scalar(kept[1][wave].k_to) + PROMPT_UNIT - 1) / PROMPT_UNIT * PROMPT_UNIT; };
+    while (after >= units_end()) {
       if (!advance(1)) {                         // no slot is left: rows of zeros, which nothing reads
         over = true;
         kr = vr = reinterpret_cast<const char *>(prompt_zeros);
@@ -595,7 +597,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
       after = scalar(kept[1][wave].k_from);
     }
     const Run &at = kept[1][wave];
-    const int kv = scalar(at.h) / P.head_tiles, keys = scalar(at.seq.keys), k0 = scalar(at.keys.first) + after + WROWS * wave, k_to = scalar(at.k_to);
+    const int kv = scalar(at.h) / P.head_tiles, keys = scalar(at.seq.keys), k0 = scalar(at.keys.first) + after + WROWS * wave;
     const int rest = keys - k0;                  // keys from the wavefront's first row on
     const uint32_t row0 = scalar(at.seq.key0) + (rest > 0 ? k0 : keys - 1);
     kr = reinterpret_cast<const char *>(P.k + (long long)kv * D) + (uint64_t)row0 * P.ldk;
@@ -606,7 +608,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
       const uint32_t last = rest > 0 ? rest - 1 : 0;
       k_most = last * P.ldk; v_most = last * P.ldv;
     } else {
-      const int whole = (rest - WROWS) / SLOT + 1, left = (k_to - after + PROMPT_UNIT - 1) / PROMPT_UNIT * PROMPT_UNIT / SLOT;
+      const int whole = (rest - WROWS) / SLOT + 1, left = (units_end() - after) / SLOT;
       here = whole < left ? whole : left;
     }
     steady = here - 1;

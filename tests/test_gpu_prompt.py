@@ -332,6 +332,19 @@ def test_prompt_attention_of_many_ragged_sequences(dn):
         check_prompt(dn, q, k, v, starts(rows), starts(keys), hq, 1, -1, 0, "bf16")
 
 
+@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (80, "f16"), (96, "bf16"), (128, "bf16"), (128, "f16"), (200, "f16"), (256, "bf16")])
+@pytest.mark.parametrize("most,left,right", [(300, -1, 0), (300, 70, 0), (700, -1, -1), (90, -1, 0)])
+def test_prompt_attention_with_many_tiles_for_every_workgroup(dn, D, dtype, most, left, right):
+    """Odd lengths, a head for every query head: tiles that end inside a stage follow one another in a workgroup."""
+    rng = np.random.default_rng(D + most)
+    rows = rng.integers(most // 2, most, 9000 // most)
+    rows[3] = 0
+    keys = rows + rng.integers(-20, 50, len(rows)).clip(-rows, None)
+    hq = 2048 // D
+    q, k, v = packed(1, rows, hq, D, dtype, 3), packed(2, keys, hq, D, dtype, 1), packed(3, keys, hq, D, dtype, 1)
+    check_prompt(dn, q, k, v, starts(rows), starts(keys), hq, hq, left, right, dtype)
+
+
 @pytest.mark.parametrize("rows", [[3, 1, 2], [60, 100, 9], [300, 20, 200]])
 def test_prompt_attention_strides_and_large_scores(dn, rows):
     """q, k and v side by side in one wide row, out in a wider row; scores up to about 100."""
