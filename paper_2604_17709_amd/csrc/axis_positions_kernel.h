@@ -36,7 +36,7 @@ __global__ __launch_bounds__(PLACE_THREADS) void axis_positions_kernel(const Axi
     const long long done = P.cached && P.cached[s] > 0 ? P.cached[s] : 0;
     r0 = r0 < 0 ? 0 : r0; r1 = r1 > P.T ? P.T : r1;
     g0 = g0 < 0 ? 0 : g0; g1 = g1 > P.n_segments ? P.n_segments : g1;
-    const int n = r1 - r0;
+    const int n = r1 > r0 ? r1 - r0 : 0;
     if (n <= (int)blockIdx.y * PLACE_THREADS) continue;          // (the same in every thread)
     long long tokens = 0, place = 0;             // of the segments so far
     // rows [from, to) of the sequence among the workgroup's

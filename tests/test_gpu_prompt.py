@@ -71,6 +71,16 @@ def test_axis_positions_of_many_requests_and_lists_that_do_not_fit(dn):
     assert np.array_equal(host(got), op.axis_positions(segments, start, rows, cached, T, np.ones((3, T))))
 
 
+def test_axis_positions_of_requests_that_end_far_ahead_of_their_start(dn):
+    """Ends of -2^31 are ends ahead of the start, whatever the start is."""
+    import torch
+    rows, T, low = [3, -2 ** 31, 2, 9], 12, -2 ** 31
+    segments = [[5, 0, 0, 0], [1, 2, 2, 1]]
+    for start in ([0, 1, 2, 2], [1, low, 0, 2]):
+        got = dn.deinfer_axis_positions(ints(segments), ints(start), ints(rows), None, T, positions=torch.full((3, T), -4, dtype=torch.int32, device="cuda"))
+        assert np.array_equal(host(got), op.axis_positions(segments, start, rows, None, T, np.full((3, T), -4)))
+
+
 def test_axis_positions_of_long_prompts(dn):
     of = [[text(70000), [40, 60, 50, 2], text(100)], [[9, 30, 30, 1]]]
     segments, start = lists(of)
