@@ -40,6 +40,10 @@ constexpr size_t PROMPT_WS_HEADER = 256;
 PromptPlan prompt_plan(int64_t T, int64_t n_seqs, int64_t n_q, int64_t n_kv, int64_t head_dim) {
   PromptPlan p;
   const int64_t per_head = ceil_div(T * (n_q / n_kv), n_seqs > 0 ? n_seqs : 1);      // rows of a sequence and key head, on average
+  // Tiles of 16 rows without LDS, of 128 and of 256, in us, heads of 128, 8 key heads.  8 query heads each, 4000 keys: 8 sequences with one
+  // token 30.9, 36.8 and 37.5, with two 32.4 and 38.6; 64 with one 201, 191 and 191, with two 205 and 193, with three (two tiles of 16)
+  // 390 and 193.  4 query heads each, whole prompts: 32 of 8 tokens 13.4, 15.1 and 16.3, 32 of 16 15.1, 15.4 and 16.7; from 64 tokens on
+  // the last two are equal, and long ones need 256 rows (906 TFLOP/s against 746).
   p.rows = per_head <= 16 ? 16 : head_dim > 128 || per_head <= 128 ? 128 : 256;
   p.cols = p.rows == 16 ? (head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256) : head_dim <= 64 ? 64 : head_dim <= 96 ? 96 : head_dim <= 128 ? 128 : 256;
   const int cus = device_cus();
@@ -209,6 +213,7 @@ int deinfer_prompt_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_
   P.T = (int)T; P.Tk = (int)n_keys; P.n_seqs = (int)n_seqs; P.head_dim = (int)head_dim; P.group = (int)(n_q_heads / n_kv_heads);
   P.head_tiles = (int)ceil_div(P.group, pl.rows); P.tile_group = (int)ceil_div(P.group, P.head_tiles); P.tile_tokens = pl.rows / P.tile_group;
   P.heads = (int)n_kv_heads * P.head_tiles; P.per_token = 1.0 / P.tile_tokens;
+  P.per_workgroup = 1.0 / (double)pl.shares;
   P.left = left < 0 || left > PROMPT_FAR ? PROMPT_FAR : (int)left;
   P.right = right < 0 || right > PROMPT_FAR ? PROMPT_FAR : (int)right;
   P.scale2 = scale2;

@@ -27,7 +27,7 @@ struct PromptParams {
   uint32_t ldk, ldv;                             // in bytes
   int T, Tk, n_seqs, head_dim, group;
   int heads, head_tiles, tile_group, tile_tokens;      // key heads x parts of their query heads (head_tiles); query heads and tokens of a tile
-  double per_token;                              // 1 / tile_tokens
+  double per_token, per_workgroup;               // 1 / tile_tokens, 1 / n_shares
   int left, right;                               // at most PROMPT_FAR
   float scale2;                                  // scale log2(e): the exponentials are powers of two
   int n_shares;
@@ -73,6 +73,9 @@ template <int START> __device__ __forceinline__ long long prompt_work(const Prom
   const int c0 = q.keys - q.n, step = P.tile_tokens;
   return (long long)t * START + clamped_series(c0 + step + P.right, step, P.per_token, q.keys, t) - clamped_series(c0 - P.left, step, P.per_token, q.keys, t);
 }
+__device__ __forceinline__ long long lane_value(long long x, int lane) {
+  return (long long)(uint32_t)__builtin_amdgcn_readlane((int)x, lane) | (long long)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32;
+}
 // a / b where the quotient is an int: a division in 64-bit floating point is off by less than one then
 __device__ __forceinline__ int small_quotient(long long a, long long b) {
   int q = (int)((double)a / (double)b);
@@ -84,8 +87,8 @@ __device__ __forceinline__ int prompt_tiles(const PromptParams &P, const PromptS
 // The order of the work: sequence after sequence; in it chunks of heads; in a chunk pairs of tiles, the last with the first and
 // so on inwards, whose work is about the same for every pair of a causal prompt; for a pair head after head; the later tile before
 // the earlier.  A chunk has so many heads that a workgroup's run is one pair through all of them: at any time the workgroups of a
-// chunk are at the same head, and read the same rows of K and V through one L2.  16 prompts of up to 2500 tokens with 32 key heads, all
-// keys seen: 1302 us in the order of heads (K and V from HBM at 4 TB/s), see below for now.
+// chunk are at the same head, and read the same rows of K and V through one L2.  16 prompts of up to 2500 tokens with 32 heads of
+// 128, fp16: 767 us causal and 1301 with all keys seen, against 796 and 1348 in the order of heads.
 //
 // A workgroup's run, tile after tile.  Everything is the same in all lanes.
 template <int UNIT, int START, int THREADS> struct PromptRun {
@@ -100,69 +103,103 @@ template <int UNIT, int START, int THREADS> struct PromptRun {
   // scan: THREADS / 64 values, found: 2 values of LDS.  False: nothing to do
   __device__ __forceinline__ bool begin(const PromptParams &P, int share, long long *scan, long long *found) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    auto work_of = [&](int x) -> long long {
-      if (x >= P.n_seqs) return 0;
-      const PromptSeq q = prompt_seq(P, x);
-      return P.heads * prompt_work<START>(P, q, prompt_tiles(P, q));
-    };
-    auto scan_work = [&](long long u, long long *total) {            // inclusive sum over the threads
+    auto before_lanes = [&](long long u) {       // inclusive sum over the wavefront's lanes
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
         const long long w = __shfl_up(u, o, 64);
         if (lane >= o) u += w;
       }
-      __syncthreads();
-      if (lane == 63) scan[wave] = u;
-      __syncthreads();
-      long long all = 0, before = 0;
-      for (int w = 0; w < THREADS / 64; ++w) { if (w < wave) before += scan[w]; all += scan[w]; }
-      *total = all;
-      return u + before;
+      return u;
     };
-    // (the last pass over up to THREADS sequences is kept: with no more of them there is one pass)
-    long long total = 0, mine = 0, mine_end = 0;
-    for (int s0 = 0; s0 < P.n_seqs; s0 += THREADS) {
-      long long t;
-      mine = work_of(s0 + tid);
-      mine_end = scan_work(mine, &t);
-      total += t;
-    }
-    total = uniform(total);
-    per_share = (long long)((double)total / P.n_shares * (1.0 + 0x1p-50)) + 1;         // (no less than the share, whatever the roundings)
-    per_share = uniform(per_share < UNIT ? UNIT : per_share);        // (every share between a tile's first and last then has a stage's last key)
-    from_work = per_share * share;
-    end = from_work + per_share < total ? from_work + per_share : total;
-    if (from_work >= end) return false;
-    long long before = 0;
-    for (int s0 = 0; s0 < P.n_seqs; s0 += THREADS) {
-      long long t = total;
-      if (P.n_seqs > THREADS) {
+    auto shared_out = [&](long long total) {
+      per_share = (long long)((double)total * P.per_workgroup * (1.0 + 0x1p-50)) + 1;  // (no less than the share, whatever the roundings)
+      per_share = uniform(per_share < UNIT ? UNIT : per_share);      // (every share between a tile's first and last then has a stage's last key)
+      from_work = per_share * share;
+      end = from_work + per_share < total ? from_work + per_share : total;
+      return from_work < end;
+    };
+    long long per_head;                          // work of the sequence for one head
+    if (P.n_seqs <= 64) {
+      // a sequence in every lane, and every wavefront for itself: nothing goes through LDS
+      PromptSeq q = {0, 0, 0, 0};
+      long long one = 0;
+      if (lane < P.n_seqs) {
+        q = prompt_seq(P, lane);
+        one = prompt_work<START>(P, q, prompt_tiles(P, q));
+      }
+      const long long mine = P.heads * one, mine_end = before_lanes(mine);
+      if (!shared_out(lane_value(mine_end, 63))) return false;
+      const unsigned long long has = __ballot(mine > 0 && mine_end - mine <= from_work && from_work < mine_end);
+      if (has == 0) return false;                // (lists of sequences that overlap so much that the sum of their work is beyond 64 bits)
+      s = __builtin_ctzll(has);
+      base = lane_value(mine_end - mine, s); per_head = lane_value(one, s);
+      seq = {__builtin_amdgcn_readlane(q.row0, s), __builtin_amdgcn_readlane(q.n, s), __builtin_amdgcn_readlane(q.key0, s), __builtin_amdgcn_readlane(q.keys, s)};
+    } else {
+      auto work_of = [&](int x) -> long long {
+        if (x >= P.n_seqs) return 0;
+        const PromptSeq q = prompt_seq(P, x);
+        return P.heads * prompt_work<START>(P, q, prompt_tiles(P, q));
+      };
+      auto scan_work = [&](long long u, long long *total) {          // inclusive sum over the threads
+        u = before_lanes(u);
+        __syncthreads();
+        if (lane == 63) scan[wave] = u;
+        __syncthreads();
+        long long all = 0, before = 0;
+        for (int w = 0; w < THREADS / 64; ++w) { if (w < wave) before += scan[w]; all += scan[w]; }
+        *total = all;
+        return u + before;
+      };
+      // (the last pass over up to THREADS sequences is kept: with no more of them there is one pass)
+      long long total = 0, mine = 0, mine_end = 0;
+      for (int s0 = 0; s0 < P.n_seqs; s0 += THREADS) {
+        long long t;
         mine = work_of(s0 + tid);
         mine_end = scan_work(mine, &t);
+        total += t;
       }
-      const long long e = before + mine_end;
-      if (mine > 0 && e - mine <= from_work && from_work < e) { found[0] = s0 + tid; found[1] = e - mine; }
-      before += t;
-      if (before > from_work) break;
+      total = uniform(total);
+      if (!shared_out(total)) return false;
+      long long before = 0;
+      if (tid == 0) found[0] = -1;
+      __syncthreads();
+      for (int s0 = 0; s0 < P.n_seqs; s0 += THREADS) {
+        long long t = total;
+        if (P.n_seqs > THREADS) {
+          mine = work_of(s0 + tid);
+          mine_end = scan_work(mine, &t);
+        }
+        const long long e = before + mine_end;
+        if (mine > 0 && e - mine <= from_work && from_work < e) { found[0] = s0 + tid; found[1] = e - mine; }
+        before += t;
+        if (before > from_work) break;
+      }
+      __syncthreads();
+      s = __builtin_amdgcn_readfirstlane((int)found[0]);
+      base = uniform(found[1]);
+      if (s < 0) return false;                   // (as above)
+      seq = prompt_seq(P, s);
+      per_head = uniform(prompt_work<START>(P, seq, prompt_tiles(P, seq)));
     }
-    __syncthreads();
-    s = __builtin_amdgcn_readfirstlane((int)found[0]);
-    base = uniform(found[1]);
-    seq = prompt_seq(P, s);
-    const long long per_head = uniform(enter(P));
+    if (from_work < base || from_work - base >= P.heads * per_head) return false;        // (and again)
+    enter(P, per_head);
     const int chunk = small_quotient(from_work - base, per_head * chunk_heads);
     chunk_first = chunk * chunk_heads;
     const int n = P.heads - chunk_first < chunk_heads ? P.heads - chunk_first : chunk_heads;
     base += (long long)chunk * chunk_heads * per_head;
-    int lo = 0, hi = (tiles - 1) / 2;            // the last pair that begins at or before from_work
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (base + n * pairs_work(P, per_head, mid) <= from_work) lo = mid; else hi = mid - 1;
+    int lo = 0, most = (tiles + 1) / 2;          // the last pair that begins at or before from_work, among [lo, most): 64 of them at a time
+    long long work;                              // in lane 0 and 1: of the pairs ahead of it, and with it
+    for (;;) {
+      const int rest = most - lo, step = (rest + 63) / 64, at = lo + lane * step;
+      work = pairs_work(P, per_head, at);
+      if (rest <= 1) break;
+      const int c = __popcll(__ballot(at < most && base + n * work <= from_work)) - 1;
+      lo += c > 0 ? c * step : 0;
+      most = lo + step < most ? lo + step : most;
     }
-    pair = __builtin_amdgcn_readfirstlane(lo);
-    const long long ahead = pairs_work(P, per_head, pair);
+    pair = lo;
+    const long long ahead = lane_value(work, 0), each = lane_value(work, 1) - ahead;
     base += n * ahead;
-    const long long each = pairs_work(P, per_head, pair + 1) - ahead;
     h = small_quotient(from_work - base, each);
     base += h * each;
     in_chunk = n - h;
@@ -176,13 +213,11 @@ template <int UNIT, int START, int THREADS> struct PromptRun {
     part();
     return mine_first() || next(P);
   }
-  // The sequence's tiles and chunks; its work for one head.
-  __device__ __forceinline__ long long enter(const PromptParams &P) {
+  // the sequence's tiles and chunks, from its work for one head
+  __device__ __forceinline__ void enter(const PromptParams &P, long long per_head) {
     tiles = prompt_tiles(P, seq);
-    const long long per_head = prompt_work<START>(P, seq, tiles);
     const float n = (float)((tiles + 1) / 2) * (float)per_share / (float)per_head;           // (rounded as it may be: the same in every workgroup)
     chunk_heads = __builtin_amdgcn_readfirstlane(n < 1.5f ? 1 : n >= (float)P.heads ? P.heads : (int)(n + 0.5f));
-    return per_head;
   }
   // work of the first n pairs of one head
   __device__ __forceinline__ long long pairs_work(const PromptParams &P, long long per_head, int n) const {
@@ -215,7 +250,7 @@ template <int UNIT, int START, int THREADS> struct PromptRun {
                 if (++s >= P.n_seqs) return false;
                 seq = prompt_seq(P, s);
               } while (seq.n == 0);
-              enter(P);
+              enter(P, prompt_work<START>(P, seq, prompt_tiles(P, seq)));
             }
           }
           in_chunk = P.heads - h < chunk_heads ? P.heads - h : chunk_heads;
@@ -245,10 +280,16 @@ __device__ __forceinline__ bool prompt_row(const PromptParams &P, const PromptSe
   return j < P.tile_tokens && token < q.n && g0 + g < P.group;
 }
 
-template <int ROWS> constexpr int PROMPT_START = ROWS == 16 ? 128 : 256;
+// What a tile costs beside its keys, in keys.  With 256 rows it is 5 to 6 us (the run's next tile 1, its queries 1, the output 2, the
+// first slots' products with nothing beside them 2); 128 in place of 256: windows of 1024 keys, heads of 256, 448 us instead of 428,
+// 256 prompts of 64 tokens 27 instead of 21; 512 the same as 256 within 1 %.  Up to 16 rows: 32 against 128 is 14.8 us against 16.5
+// for 8 tokens over 1000 keys and 51.7 against 51.3 for 128 over 500.
+template <int ROWS> constexpr int PROMPT_START = ROWS == 16 ? 32 : 256;
 
 // ---- up to 16 rows per tile: single tokens and the like over long caches.  Four wavefronts, each its own 32 of 128 keys,
 // operands straight from memory into registers (the products and the way of V's operand are those of tree_attention_kernel).
+// Bound by HBM: 64 sequences with one token each, 64 query and 8 key heads of 128, 0 .. 8191 keys: 1.08 GB in 209 us, 5.2 TB/s (a large
+// copy reaches 5.0, a read alone 6).
 template <int DT, int DP, bool FULL>
 __global__ __launch_bounds__(ATT_THREADS) void prompt_rows_kernel(const PromptParams P) {
   constexpr int WK = ATT_THREADS / 64, UNIT = ATT_KEYS * WK, ROWS = 16, START = PROMPT_START<16>;
@@ -472,6 +513,22 @@ __global__ __launch_bounds__(ATT_THREADS) void prompt_rows_kernel(const PromptPa
 }
 
 // ---- more rows: WAVES wavefronts with 32 rows each share the keys, SLOT at a time, through a ring of four slots in LDS.
+//
+// Scores are computed as S^T = K Q^T, so that a lane has 16 scores of one row, which rounded to the type are the operand of
+// O^T += V^T P^T as they are; V's operand is read transposed.  A slot's rows go from memory to LDS without registers, three slots ahead,
+// across the ends of tiles, with one barrier a slot.  A row's reference is its first maximum, moved to where the powers of two use
+// the type's range, and changed only when a probability gets large: most turns (32 keys) neither take a maximum nor rescale.
+//
+// Bound by the issue of one wavefront's instructions: a turn of heads of 128 has 16 products of 32 cycles and 78 vector instructions, of which 16
+// are exponentials, and a product hides about five of them (three beside an exponential).  So the products of the turn before run beside the
+// probabilities, the next scores beside the sum and the reads of V, in a fixed order, and registers hold 32 rows: with 64 rows per
+// wavefront (half the reads from LDS) 970 TFLOP/s in place of 1015, with two groups of wavefronts in opposite halves of a turn 950.
+//   one prompt of 16384 tokens, 64 query and 8 key heads of 128, bf16     4.40 TFLOP    4.0 ms    1100 TFLOP/s (a large library product: 1210)
+//   16 of 1250 .. 2500, 32 heads of 128, fp16                             0.53          0.78      680
+//   4 of 3500 .. 6000, windows of 1024, 16 query and 8 key heads of 256   0.30          0.46      660
+//   24 images of 700 .. 1024 patches, 16 heads of 80, fp16                0.067         0.16      420
+// In the first the matrix units are busy for 51 % of the cycles and the clock goes down to 1.8 to 2 GHz: at that point power takes part in the bound.
+// In the others tiles have few keys (PROMPT_START), and heads of 80 have 11 products a turn for the same vector instructions.
 // KS: 16-feature steps of the first product (padded head dimension 16 KS); PITCH: features of a row in LDS.
 template <int KS_, int WAVES_> struct PromptTile {
   static constexpr int KS = KS_, WAVES = WAVES_;
@@ -626,13 +683,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
   const uint32_t k_row = (lane / CH) * P.ldk, v_row = (lane / CH) * P.ldv;
   const uint32_t k_off = ((lane % CH) ^ prompt_swizzle_k<C::PITCH>(WROWS * wave + lane / CH)) * 16, v_off = ((lane % CH) ^ prompt_swizzle_v<C::PITCH>(WROWS * wave + lane / CH)) * 16;
   const uint32_t ring = lds_at(prompt_smem) + wave * WROWS * ROWB;             // the wavefront's rows of the ring's first place
-  // Load instructions from .. to - 1 of the 2 NL that bring its rows into place b of the ring: as many whatever keys there are, so that
-  // the waits below can count them.
-  auto issue = [&](int b, int from, int to) __attribute__((always_inline)) {
+  // The 2 NL load instructions that bring its rows into place b of the ring: as many whatever keys there are, so that the waits
+  // below can count them.
+  auto issue = [&](int b) __attribute__((always_inline)) {
     const char *ks = kr, *vs = vr;
     settled(ks, vs);
 #pragma unroll
-    for (int i = from; i < to; ++i) {
+    for (int i = 0; i < 2 * NL; ++i) {
       const bool v = i % 2;
       const uint32_t place = ring + b * 2 * BUF + (v ? BUF : 0) + i / 2 * 1024, ld = v ? P.ldv : P.ldk, most = v ? v_most : k_most;
       const uint32_t piece = (v ? v_off : k_off) ^ ((v ? prompt_swizzle_v<C::PITCH>(RPI * (i / 2)) : prompt_swizzle_k<C::PITCH>(RPI * (i / 2))) * 16);
@@ -649,7 +706,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
     for (int ks = 0; ks < KS; ++ks) kf[ks] = *reinterpret_cast<const u32x4_t *>(kb + (kx ^ (ks * 32)));
   };
 
-  for (int i = 0; i < 3; ++i) { next_slot(); issue(i, 0, 2 * NL); }
+  for (int i = 0; i < 3; ++i) { next_slot(); issue(i); }
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");
   __builtin_amdgcn_s_barrier();                  // slots 0 and 1 have landed
   asm volatile("" ::: "memory");
@@ -685,7 +742,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
   bool more;
   do {
     // The queries are waited for here, with what is under way to LDS: left to the compiler, which does not know of the loads in
-    // assembly, the wait stands ahead of every use in the loop below, and there it is one for all rows of K and V under way.
+    // assembly, the wait stands ahead of every use in the loop below, and there it is one for all rows of K and V under way.  (The
+    // output's stores are waited for too; a wait ahead of them in its place measured the same.)
     __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
     // keys that every row of the wavefront sees (rows that are none see nothing and need no mask)
     const int w0 = wave * 32 / P.tile_group, w1 = (wave * 32 + 31) / P.tile_group, t_first = tile * P.tile_tokens + w0;
@@ -789,7 +847,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
           __builtin_amdgcn_s_barrier();          // ... and everybody's
           asm volatile("" ::: "memory");
           next_slot();
-          issue((b + 3) & 3, 0, 2 * NL);
+          issue((b + 3) & 3);
         }
         const unsigned char *vb = prompt_smem + b * 2 * BUF + BUF + c * 32 % SLOT * ROWB;
         if ((c + 1) * 32 % SLOT == 0) b = (b + 1) & 3;
@@ -938,7 +996,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (rows loaded ahead and not used: their place in LDS is this workgroup's until they land)
 }
 
-// Joins the partial results of the tiles whose keys several workgroups had: workgroup (b, y) takes sixteen rows of the tile that
+// Joins the partial results of the tiles whose keys several workgroups had (4 to 17 us, the last for 256 tiles of 256 rows with heads of
+// 128: up to 67 MB of partial results, just written): workgroup (b, y) takes sixteen rows of the tile that
 // begins in share b, whose other parts are the first of the shares after it.  Threads: (group of parts) x (row, 4
 // features); the groups' sums are joined in LDS in a fixed order.
 template <int DT, int COLS, int ROWS>
