@@ -488,7 +488,8 @@ int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_he
  *   out[t, h] = sum_j p_j v_j, p = softmax over the keys j that row t sees of scale (q[t, h] . k_j)
  * where query head h reads key head h / (n_q_heads / n_kv_heads).
  *   q_start, k_start: device int32 [n_seqs + 1]: first row of every sequence in q and out, in k and v, and the end of the last; k_start
- *                   NULL: q_start.  Row i of a sequence with n rows and m keys stands at p = m - n + i (the last row at the last key)
+ *                   NULL: q_start.  What lies outside the tensors is cut off; sequences do not share rows of out (the lists do not
+ *                   decrease).  Row i of a sequence with n rows and m keys stands at p = m - n + i (the last row at the last key)
  *                   and sees its keys j, p - left <= j <= p + right; a negative side has no bound (causal: left = -1, right = 0).  A row that sees
  *                   no key gives zeros; so does one whose scores are all minus infinity.  What a row does not see has no
  *                   influence, infinities and NaN included.

@@ -342,6 +342,40 @@ def test_prompt_attention_of_many_ragged_sequences(dn):
         check_prompt(dn, q, k, v, starts(rows), starts(keys), hq, 1, -1, 0, "bf16")
 
 
+@pytest.mark.parametrize("n_seqs", [1, 2, 63, 64, 65, 128, 129])
+@pytest.mark.parametrize("most,hq", [(2, 4), (40, 4), (200, 2)])
+def test_prompt_attention_of_as_many_sequences_as_a_wavefront_has_lanes(dn, n_seqs, most, hq):
+    """Sequences without rows, without keys or with neither among them, also the first and the last."""
+    rng = np.random.default_rng(n_seqs)
+    rows, keys = rng.integers(0, most, n_seqs), rng.integers(0, 300, n_seqs)
+    rows[0], rows[n_seqs // 2] = 0, most
+    keys[n_seqs // 3] = 0
+    q, k, v = packed(4, rows, 2 * hq, 64, "f16", 2), packed(5, keys, 2, 64, "f16", 5), packed(6, keys, 2, 64, "f16", 5)
+    check_prompt(dn, q, k, v, starts(rows), starts(keys), 2 * hq, 2, -1, 0, "f16")
+
+
+@pytest.mark.parametrize("n", [70, 20000])
+def test_pairs_of_tiles_beyond_a_wavefront(dn, n):
+    """A sequence with more pairs of tiles than a wavefront has lanes: every row with its own key alone, and with a few around it."""
+    import torch
+    hq, D = 16, 64
+    rows = [n, 3, n // 3]
+    q, k, v = (packed(s, rows, h, D, "bf16") for s, h in ((7, hq), (8, 1), (9, 1)))
+    ws = dn.Workspace(dn.deinfer_prompt_attention_workspace_bytes(sum(rows), 3, hq, 1, D))
+    got = dn.deinfer_prompt_attention(q, k, v, ints(starts(rows)), ws, hq, 1, left=0, right=0)
+    assert torch.equal(got.view(-1, hq, D), v.view(-1, 1, D).expand(-1, hq, D))          # p = 1: the value itself
+    got = dn.deinfer_prompt_attention(q, k, v, ints(starts(rows)), ws, hq, 1, left=5, right=2).view(-1, hq, D).double()
+    of = torch.repeat_interleave(torch.arange(3, device="cuda"), torch.tensor(rows, device="cuda"))
+    at = torch.arange(sum(rows), device="cuda")[:, None] + torch.arange(-5, 3, device="cuda")          # the keys of every row
+    held = at.clamp(0, sum(rows) - 1)
+    seen = (at == held) & (of[held] == of[:, None])
+    x = (q.double().view(-1, 1, hq, D) * k.double()[held][:, :, None]).sum(3) * D ** -0.5
+    prob = torch.softmax(x.masked_fill(~seen[:, :, None], -float("inf")), 1)[:, :, :, None]
+    vs = v.double()[held][:, :, None]
+    want, size = (prob * vs).sum(1), (prob * vs.abs()).sum(1)
+    assert bool(((got - want).abs() <= HALF["bf16"] * (want.abs() + size) * 1.01 + 4e-4 * size).all())
+
+
 @pytest.mark.parametrize("D,dtype", [(64, "bf16"), (80, "f16"), (96, "bf16"), (128, "bf16"), (128, "f16"), (200, "f16"), (256, "bf16")])
 @pytest.mark.parametrize("most,left,right", [(300, -1, 0), (300, 70, 0), (700, -1, -1), (90, -1, 0)])
 def test_prompt_attention_with_many_tiles_for_every_workgroup(dn, D, dtype, most, left, right):
