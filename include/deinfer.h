@@ -492,7 +492,8 @@ int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_he
  *                   decrease).  Row i of a sequence with n rows and m keys stands at p = m - n + i (the last row at the last key)
  *                   and sees its keys j, p - left <= j <= p + right; a negative side has no bound (causal: left = -1, right = 0).  A row that sees
  *                   no key gives zeros; so does one whose scores are all minus infinity.  What a row does not see has no
- *                   influence, infinities and NaN included.
+ *                   influence, infinities and NaN included.  An infinite value that it sees makes an infinity, or no number where
+ *                   the value's probability is so small that it counts as 0.
  *   q, out: T x (n_q_heads head_dim), pitches ldq, ldo; k, v: n_keys x (n_kv_heads head_dim), pitches ldk, ldv.  16-byte aligned,
  *                   pitches multiples of 8.  out must not overlap the others.
  *   dtype: bf16 or fp16.  head_dim: a multiple of 8, at most 256.  scale: a normal positive number of fp32, with 1 / ln 2 on it too.

@@ -780,8 +780,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
         x = mfma32<DT>(kf[ks], qf[ks], x);
     };
     // Values that are infinite or NaN among the 32 keys from k0 on, some of which some row does not see: 0 x infinity is no number.  They
-    // are taken out of the operand, and where a row sees one, it is added to the row's output as what it is.
-    auto odd_values = [&](int k0) __attribute__((always_inline)) {
+    // are taken out of the operand, and where a row sees one, its product with the row's probability is added to the row's output: an
+    // infinite value's is no number where the probability is 0, as in turns that every row sees, and what the value is elsewhere.
+    auto odd_values = [&](int k0, const u32x4_t (&prob)[2]) __attribute__((always_inline)) {
       constexpr uint32_t INF = DT == DT_F16 ? 0x7c007c00u : 0x7f807f80u, ONE = DT == DT_F16 ? 0x3c00u : 0x3f80u;
       uint32_t most = 0;
 #pragma unroll
@@ -801,21 +802,25 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
       for (int f = 0; f < NF; ++f) {
         asm volatile("" : "+v"(vf[f][0]), "+v"(vf[f][1]));         // (nothing of this is kept from the test above, or for the next block)
 #pragma unroll 1
-        for (int kind = 0; kind < 3; ++kind) {   // infinity, minus infinity, NaN
+        for (int kind = 0; kind < 4; ++kind) {   // infinity, minus infinity, NaN, an infinity of either sign (or NaN) beside a probability of 0
           const uint32_t add = kind == 0 ? 0x7f800000u : kind == 1 ? 0xff800000u : 0x7fc00000u;
-          const uint32_t hide = kind == 2 ? 0x7fff7fffu : 0xffffffffu, other = kind == 0 ? INF : kind == 1 ? INF | 0x80008000u : 0u;
+          const uint32_t hide = kind >= 2 ? 0x7fff7fffu : 0xffffffffu, other = kind == 0 ? INF : kind == 1 ? INF | 0x80008000u : 0u;
+          const uint32_t under = kind == 2 ? INF : INF - 0x00010001u;
+          const uint32_t all = kind == 2 ? 0xffffffffu : 0u, turned = kind == 3 ? 0xffffffffu : 0u;
           f32x16_t n;
 #pragma unroll
           for (int i = 0; i < 16; ++i) n[i] = 0.0f;
 #pragma unroll
           for (int kk = 0; kk < 2; ++kk) {
-            u32x4_t one;
+            u32x4_t one, mine;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {        // (arithmetic on pairs: 1 where it is one of the kind)
               const uint32_t v = (vf[f][kk][w] & hide) ^ other;
-              one[w] = times_pair(kind == 2 ? smaller_pair(minus_pair(v, INF), 0x00010001u) : smaller_pair(v, 0x00010001u) ^ 0x00010001u, ONE * 0x00010001u);
+              one[w] = times_pair(kind >= 2 ? smaller_pair(minus_pair(v, under), 0x00010001u) : smaller_pair(v, 0x00010001u) ^ 0x00010001u, ONE * 0x00010001u);
+              const uint32_t some = times_pair(smaller_pair(prob[kk][w] & 0x7fff7fffu, 0x00010001u), 0xffffffffu);       // (all ones where the probability is not 0)
+              mine[w] = see[kk][w] & ((some ^ turned) | all);
             }
-            n = mfma32<DT>(one, see[kk], n);
+            n = mfma32<DT>(one, mine, n);
           }
 #pragma unroll
           for (int i = 0; i < 16; ++i) {       // (n: how many the row sees)
@@ -856,7 +861,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
         if (LEAVE && (k > some_high + 32 || k + 63 < some_low)) continue;
         const bool masked = k + 31 > all_high || k < all_low;
         if (__builtin_expect(masked || hidden, 0)) {
-          if (hidden) odd_values(k - 32);
+          if (hidden) odd_values(k - 32, pf[1 - c]);
           if (masked) {
             const int up = high - k - 4 * half, down = low - k - 4 * half;
 #pragma unroll
@@ -953,7 +958,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void prompt_tile_kernel(cons
     }
     const int k_end = k_first + (k_last - k_first + PROMPT_UNIT - 1) / PROMPT_UNIT * PROMPT_UNIT - 32;        // of the last turn
     const bool rest = k_first < k_last && (!LEAVE || k_end <= some_high);        // the last turn's values are to be added
-    if (rest && hidden) odd_values(k_end);
+    if (rest && hidden) odd_values(k_end, pf[1]);
 
     // ---- out: to the rows, where this workgroup had all their keys, else to the workspace; the next tile's queries are asked for
     // ahead of that
