@@ -481,7 +481,7 @@ int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_he
  *   positions:      device int32 [n_axes][pos_pitch]; pair i is rotated by positions[axis_of[i]][t] freqs[i].  axis_of: device uint8
  *                   [rot_dim / 2] (may be NULL with one axis; an axis that there is not counts as 0).
  * Everything else as of deinfer_rope_store: pitches, slots, outputs in place.  Sums and products in fp32 (a sum out of fp32's
- * range in 64 bits), angles in double precision, one rounding.  head_dim <= DEINFER_NORM_MAX_DIM, T <= 2^28.
+ * range in 64 bits, with eps as it is), angles in double precision, one rounding.  head_dim <= DEINFER_NORM_MAX_DIM, T <= 2^28.
  *
  * deinfer_prompt_attention: attention of packed sequences: prompts, chunks behind others' keys, images whose patches all see
  * each other, single tokens over rebuilt keys and values.

@@ -24,8 +24,8 @@ struct NormRopeParams {
   const void *q_weight, *k_weight;               // [head_dim], or NULL: that side is not normed
   const uint8_t *axis_of;                        // [rot_dim / 2], or NULL: axis 0
   long long pos_pitch;
+  double eps;
   int n_axes;
-  float eps;
   int lanes;                                     // of a head: a power of two, at most 64
 };
 
@@ -83,7 +83,8 @@ template <typename TE, int VE, bool WHOLE> struct Elems {
 };
 
 // What a head's elements are multiplied by, from the sum of their squares over the lanes of the head: 1 / sqrt(mean + eps).  Where the
-// fp32 sum is out of its comfortable range (elements of 1e19 and more, or all tiny) the factor comes from a sum in 64 bits.
+// fp32 sum is out of its comfortable range (elements of 1e19 and more, or all tiny: there an eps that fp32 has no bits for counts too)
+// the factor comes from a sum in 64 bits.
 struct HeadScale {
   float f;
   double d;
@@ -174,7 +175,8 @@ __global__ __launch_bounds__(ROPE_THREADS) void norm_rope_store_kernel(const Nor
       sum = squares(sum);
       for (int c = lane + lanes; c < pieces; c += lanes) { fetch(c); sum = squares(sum); }
       sum = lanes_sum(sum, lanes);
-      scale.wide = !(sum > 1e-30f && sum < 1e38f);
+      const float mean = sum / (float)D + (float)Q.eps;
+      scale.wide = !(sum > 1e-30f && sum < 1e38f && mean < 1e38f);
       if (scale.wide) {
         double wide = 0.0;
         for (int c = lane; c < pieces; c += lanes) {
@@ -182,9 +184,9 @@ __global__ __launch_bounds__(ROPE_THREADS) void norm_rope_store_kernel(const Nor
 #pragma unroll
           for (int e = 0; e < VE; ++e) wide += (double)a.x[e] * a.x[e] + (INTER ? 0.0 : (double)b.x[e] * b.x[e]);
         }
-        scale.d = 1.0 / sqrt(lanes_sum(wide, lanes) / D + (double)Q.eps);
+        scale.d = 1.0 / sqrt(lanes_sum(wide, lanes) / D + Q.eps);
       } else {
-        scale.f = rsqrtf(sum / (float)D + Q.eps);
+        scale.f = rsqrtf(mean);
       }
       if (pieces > lanes || scale.wide) {
         if (lane < pieces) fetch(lane);

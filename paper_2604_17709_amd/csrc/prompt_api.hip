@@ -153,7 +153,7 @@ int deinfer_norm_rope_store(const void *q, int64_t ldq, int64_t n_q_heads, const
   P.T = (int)T; P.n_q = have_q ? (int)n_q_heads : 0; P.n_kv = have_k ? (int)n_kv_heads : 0; P.n_v = have_v ? (int)n_kv_heads : 0;
   P.head_dim = (int)head_dim; P.rot_dim = turn ? (int)rot_dim : 0; P.magnitude = (float)magnitude;
   Q.q_weight = have_q ? q_weight : nullptr; Q.k_weight = have_k ? k_weight : nullptr;
-  Q.axis_of = n_axes > 1 ? axis_of : nullptr; Q.pos_pitch = pos_pitch; Q.n_axes = (int)n_axes; Q.eps = (float)eps;
+  Q.axis_of = n_axes > 1 ? axis_of : nullptr; Q.pos_pitch = pos_pitch; Q.n_axes = (int)n_axes; Q.eps = eps;
   const int pieces = (inter ? P.rot_dim : P.rot_dim / 2) / ve + (P.head_dim - P.rot_dim) / ve;
   Q.lanes = 1;
   while (Q.lanes < pieces && Q.lanes < kWave) Q.lanes *= 2;

@@ -3,8 +3,8 @@ import numpy as np
 import pytest
 
 from oracle import prompt as op
-from test_gpu_cache_step import HALF, dn, ints, kind_of, wide  # noqa: F401
-from test_gpu_prompt import packed
+from test_gpu_cache_step import HALF, dn, host, ints, kind_of, normal, wide  # noqa: F401
+from test_gpu_prompt import angles_of, check_norm, packed
 
 pytestmark = pytest.mark.gpu
 
@@ -32,3 +32,16 @@ def test_seen_infinities_whose_probability_is_nothing(dn, dtype, right, n, hq, D
     assert np.array_equal(np.isnan(got), hit), np.argwhere(np.isnan(got) != hit)[:5]
     tol = HALF[dtype] * (np.abs(ref) + size) * 1.01 + 4e-4 * size + (n * 2.0 ** -25 * np.max(size) if dtype == "f16" else 0.0)
     assert np.all((np.abs(got - ref.reshape(hit.shape)) <= tol.reshape(hit.shape))[~hit])
+
+
+# ------------------------------------------------------------------ norms: eps of any size
+@pytest.mark.parametrize("size,eps", [(0.0, 1e-50), (1e-28, 1e-50), (1e-30, 1e-46), (3e-23, 1e-46), (3e18, 3.4e38), (0.0, 3.4e38), (1e-12, 1e-40), (1.0, 1e-60)])
+@pytest.mark.parametrize("D", [8, 64])
+def test_norms_with_an_eps_beyond_fp32(dn, size, eps, D):
+    """eps is a 64-bit number: one that fp32 has no bits for is not nothing, and one near its end does not make the sum infinite."""
+    import torch
+    T, H = 5, 3
+    x = torch.tensor(np.clip(normal(9, T, H * D), -1.0, 1.0) * size, device="cuda").float()
+    w, f, pos = torch.ones(D, device="cuda"), torch.tensor(10000.0 ** (-2.0 * np.arange(D // 2) / D), device="cuda"), np.arange(T)
+    y = dn.deinfer_norm_rope_store(x.clone(), None, None, ints(pos), f, H, 0, D, q_weight=w, eps=eps)[0]
+    check_norm(wide(y), wide(x), H, wide(w), eps, angles_of(pos[None], np.zeros(D // 2), host(f)), 1.0, False, "f32")
