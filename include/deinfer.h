@@ -457,7 +457,8 @@ int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_he
 /*
  * Between the projections of a prompt: positions of several axes, norms of queries and keys with their rotation, and
  * attention over the rows of keys and values as the projections write them, with no pages between.  Lengths and positions are in device
- * memory, so that one captured graph serves every step; rows behind the last sequence's are padding and left as they are.
+ * memory, so that one captured graph serves every step; rows behind the last sequence's are padding, and positions and attention leave
+ * them as they are.  deinfer_norm_rope_store takes no lengths and knows padding by its slots: without slots it writes all T rows.
  *
  * deinfer_axis_positions: positions (time, height, width) of a step's tokens, for requests that mix text with images and video.
  *   segments:       device int32 [n_segments][4], 16-byte aligned: {t, h, w, step}.  h or w not positive: text of t tokens; else a
@@ -480,7 +481,9 @@ int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_he
  *                   w x / sqrt(mean x^2 + eps), its elements from rot_dim on too; values are copied.
  *   positions:      device int32 [n_axes][pos_pitch]; pair i is rotated by positions[axis_of[i]][t] freqs[i].  axis_of: device uint8
  *                   [rot_dim / 2] (may be NULL with one axis; an axis that there is not counts as 0).
- * Everything else as of deinfer_rope_store: pitches, slots, outputs in place.  Sums and products in fp32 (a sum out of fp32's
+ * Everything else as of deinfer_rope_store: pitches, slots, outputs in place.  A row whose slot is outside [0, n_slots)
+ * (deinfer_kv_step makes -1 for padding) is left as it is, its queries too, also with k and v NULL; without slots every one of the T
+ * rows is normed and written, in place at every replay of a graph again.  Sums and products in fp32 (a sum out of fp32's
  * range in 64 bits, with eps as it is), angles in double precision, one rounding.  head_dim <= DEINFER_NORM_MAX_DIM, T <= 2^28.
  *
  * deinfer_prompt_attention: attention of packed sequences: prompts, chunks behind others' keys, images whose patches all see

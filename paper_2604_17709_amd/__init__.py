@@ -818,7 +818,8 @@ def deinfer_rope_axes(rot_dim: int, pairs: Sequence[int], turns: bool = False):
 def deinfer_norm_rope_store(q, k, v, positions, freqs, n_q_heads: int, n_kv_heads: int, head_dim: int, q_weight=None, k_weight=None, eps: float = 1e-6,
                             axis_of=None, interleaved: bool = False, magnitude: float = 1.0, slots=None, q_out=None, k_out=None, v_out=None, stream=None):
     """``deinfer_rope_store`` with every head of q and k normed by its root mean square ahead of the rotation (where its weight
-    [head_dim] is given), and positions of several axes: int32 [n_axes, rows] with axis_of, uint8 device tensor [rot_dim / 2]."""
+    [head_dim] is given), and positions of several axes: int32 [n_axes, rows] with axis_of, uint8 device tensor [rot_dim / 2].  Rows
+    without a slot are left out; without ``slots`` every row is written."""
     import torch
     if q is None and k is None and v is None:
         return q_out, k_out, v_out

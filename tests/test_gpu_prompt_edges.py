@@ -4,7 +4,7 @@ import pytest
 
 from oracle import prompt as op
 from test_gpu_cache_step import HALF, dn, host, ints, kind_of, normal, wide  # noqa: F401
-from test_gpu_prompt import angles_of, check_norm, packed
+from test_gpu_prompt import angles_of, check_norm, norm_case, packed
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +45,46 @@ def test_norms_with_an_eps_beyond_fp32(dn, size, eps, D):
     w, f, pos = torch.ones(D, device="cuda"), torch.tensor(10000.0 ** (-2.0 * np.arange(D // 2) / D), device="cuda"), np.arange(T)
     y = dn.deinfer_norm_rope_store(x.clone(), None, None, ints(pos), f, H, 0, D, q_weight=w, eps=eps)[0]
     check_norm(wide(y), wide(x), H, wide(w), eps, angles_of(pos[None], np.zeros(D // 2), host(f)), 1.0, False, "f32")
+
+
+# ------------------------------------------------------------------ rows behind the last sequence
+def test_norms_of_a_captured_step_leave_rows_without_a_slot(dn):
+    """A graph replayed for steps of fewer and fewer tokens, slots from the step: what lies behind the last sequence's rows stays as it is in the
+    queries too.  Without slots every row of the buffers is written."""
+    import torch
+    rows, hq, hk, D, bt, n_pool = 40, 4, 2, 64, 8, 16
+    q, k, v, (qw, kw) = norm_case("bf16", rows, hq, hk, D, 0, seed=8)
+    f = torch.tensor(10000.0 ** (-2.0 * np.arange(D // 2) / D), device="cuda")
+    cached, new, table = ints([0, 0]), ints([0, 0]), torch.full((2, 8), -1, dtype=torch.int32, device="cuda")
+    free = ints(np.arange(n_pool))
+    step = dn.deinfer_kv_step(cached, new, table, free, bt, n_pool, rows)
+    pools = [torch.zeros(n_pool * bt, hk * D, dtype=q.dtype, device="cuda") for _ in range(2)]
+    to, straight = torch.zeros_like(q), torch.zeros_like(q)
+
+    def call():
+        dn.deinfer_kv_step(cached, new, table, free, bt, n_pool, rows, out=step)
+        dn.deinfer_norm_rope_store(q, k, v, step.positions, f, hq, hk, D, q_weight=qw, k_weight=kw, slots=step.slots, q_out=to, k_out=pools[0], v_out=pools[1])
+        dn.deinfer_norm_rope_store(q, None, None, step.positions, f, hq, 0, D, q_weight=qw, q_out=straight)
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for lengths in ([20, 20], [9, 14], [1, 1], [0, 0], [30, 1]):
+        new.copy_(ints(lengths))
+        to.fill_(float("nan")), straight.fill_(float("nan"))
+        for p in pools:
+            p.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        n = sum(lengths)
+        pos = np.r_[np.concatenate([np.arange(m) for m in lengths]), np.zeros(rows - n)]
+        angles = angles_of(pos[None], np.zeros(D // 2), host(f))
+        check_norm(wide(straight), wide(q), hq, wide(qw), 1e-6, angles, 1.0, False, "bf16")
+        assert torch.equal(to[:n], straight[:n]) and bool(torch.isnan(to[n:]).all())
+        slots = host(step.slots)
+        assert np.all(slots[:n] >= 0) and np.all(slots[n:] == -1)
+        unused = np.setdiff1d(np.arange(n_pool * bt), slots[:n])
+        assert bool(torch.isnan(pools[0][unused]).all()) and bool(torch.isnan(pools[1][unused]).all())
+        assert torch.equal(pools[1][slots[:n]], v[:n])
