@@ -860,7 +860,7 @@ def deinfer_prompt_attention_workspace_bytes(rows: int, n_seqs: int, n_q_heads: 
 def deinfer_prompt_attention(q, k, v, q_start, ws: Workspace, n_q_heads: int, n_kv_heads: int, k_start=None, scale: Optional[float] = None, left: int = -1,
                              right: int = 0, out=None, stream=None):
     """Attention of packed sequences: q [rows, n_q_heads * head_dim]; k, v [key rows, n_kv_heads * head_dim]; q_start, k_start: int32
-    [n_seqs + 1] (k_start None: q_start).  A row sees the keys from ``left`` before its place to ``right`` behind it, the last row
+    [n_seqs + 1] (k_start None: q_start); a gap between the keys of two sequences is a sequence without rows.  A row sees the keys from ``left`` before its place to ``right`` behind it, the last row
     standing at the last key; negative: no bound.  Rows behind the last sequence's keep what ``out`` holds (a new one:
     whatever its memory held)."""
     rows, cols, ldq = _matrix(q, "q")

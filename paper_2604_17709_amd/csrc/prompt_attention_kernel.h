@@ -1,5 +1,6 @@
 // Attention of packed prompts over packed keys and values: rows of q, k and v as the projections write them (or keys
-// and values rebuilt from the low-rank cache), sequence after sequence, no pages.
+// and values rebuilt from the low-rank cache), sequence after sequence, no pages.  Gaps between the keys of sequences, as the
+// rebuilt cache has them, are sequences without rows, which have no tiles and no work.
 //
 // Token i of a sequence with n rows and K keys stands at p = K - n + i and sees the keys j with p - left <= j <= p + right,
 //   o = sum_j exp(x_j - max x) v_j / sum_j exp(x_j - max x),   x_j = scale q . k_j,

@@ -88,3 +88,55 @@ def test_norms_of_a_captured_step_leave_rows_without_a_slot(dn):
         unused = np.setdiff1d(np.arange(n_pool * bt), slots[:n])
         assert bool(torch.isnan(pools[0][unused]).all()) and bool(torch.isnan(pools[1][unused]).all())
         assert torch.equal(pools[1][slots[:n]], v[:n])
+
+
+# ------------------------------------------------------------------ keys with gaps between sequences
+@pytest.mark.parametrize("cached,new", [([37, 5, 90], [2, 1, 3]), ([0, 15, 33, 1], [1, 1, 1, 1]), ([40, 0, 7], [60, 33, 20]), ([16, 30], [16, 2])])
+@pytest.mark.parametrize("hq,hk,D", [(4, 2, 128), (8, 1, 64)])
+def test_keys_rebuilt_from_the_low_rank_cache(dn, cached, new, hq, hk, D):
+    """Plan, compacting copies, keys rebuilt and rotated, values rebuilt: every sequence begins at a block, so that there is a gap behind most,
+    a sequence without rows.  Against the attention through the remapped table, and in 64 bits."""
+    import torch
+    bt, r, d_in, n_pool, buf_blocks, n = 16, 40, 64, 32, 20, len(cached)
+    total, T = [c + m for c, m in zip(cached, new)], sum(new) + 3
+    pair = lambda s: dn.deinfer_pack_factors(dn.raw_pair(torch.tensor(normal(s, d_in, r) / 8, device="cuda").to(torch.bfloat16),
+                                                        torch.tensor(normal(s + 1, r, hk * D) / 6, device="cuda").to(torch.bfloat16)))
+    fk, fv = pair(30), pair(32)
+    pools = [torch.tensor(normal(34 + i, n_pool * bt, r), device="cuda").to(torch.bfloat16) for i in range(2)]
+    blocks = [-(-c // bt) for c in total]
+    table = np.full((n, 9), -1)
+    ids = np.random.default_rng(2).permutation(n_pool)
+    for s in range(n):
+        table[s, :blocks[s]] = ids[sum(blocks[:s]):sum(blocks[:s + 1])]
+    lengths = ints(total)
+    plan, remap, pos = dn.deinfer_kv_compact_plan_device(ints(table), lengths, n_pool, buf_blocks, bt)
+    bufs = [torch.full((buf_blocks * bt, r), 50.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for p, b in zip(pools, bufs):
+        dn.deinfer_kv_compact_copy(p, bt * r * 2, plan, b)
+    ws = dn.Workspace(max(dn.deinfer_workspace_bytes(buf_blocks * bt, [fk, fv]), dn.deinfer_tree_attention_workspace_bytes(T, n, hq, hk, D),
+                          dn.deinfer_prompt_attention_workspace_bytes(T, 2 * n, hq, hk, D)))
+    keys = dn.deinfer_lowrank_up_rope(bufs[0], fk, dn.deinfer_rope_table(pos, D), ws)
+    values = dn.deinfer_lowrank_up(bufs[1], fv, ws)
+    q = packed(50, new, hq, D, "bf16", 3)
+    row_start = ints(starts(new))
+    paged = dn.deinfer_tree_attention(q, keys, values, remap, row_start, ints(cached), ws, hq, hk, bt)
+    # sequence 2 s: the rows and keys of s; sequence 2 s + 1: no rows, and the rest of its last block
+    q_start = row_start[torch.tensor([0] + [s for s in range(1, n + 1) for _ in range(2)], device="cuda")].contiguous()
+    block_end = torch.cumsum((lengths + bt - 1) // bt * bt, 0).int()
+    first = torch.cat([torch.zeros_like(block_end[:1]), block_end[:-1]])
+    k_start = torch.cat([torch.stack([first, first + lengths], 1).flatten(), block_end[-1:]]).contiguous()
+    out = torch.full((T, hq * D), 3.0, dtype=torch.bfloat16, device="cuda")
+    dn.deinfer_prompt_attention(q, keys, values, q_start, ws, hq, hk, k_start=k_start, out=out)
+    got, qh, vh = wide(out), np.nan_to_num(wide(q)), wide(values)
+    args = (host(q_start), host(k_start), hq, hk, -1, 0, D ** -0.5, np.full((T, hq * D), 3.0))
+    ref, size = op.attention(qh, wide(keys), vh, *args), op.attention(qh, wide(keys), np.abs(vh), *args)
+    rows = sum(new)
+    assert np.all((np.abs(got - ref) <= HALF["bf16"] * (np.abs(ref) + size) * 1.01 + 4e-4 * size)[:rows])
+    assert np.all(np.abs(got - wide(paged))[:rows] <= 2 * (HALF["bf16"] * (np.abs(ref) + size) * 1.01 + 4e-4 * size)[:rows])
+    assert np.all(got[rows:] == 3.0)
+    # (what stands in the gaps is not seen)
+    for b, t in ((values, float("inf")), (keys, float("nan"))):
+        for s in range(n):
+            b[int(host(first)[s]) + total[s]:int(host(block_end)[s])] = t
+    again = dn.deinfer_prompt_attention(q, keys, values, q_start, ws, hq, hk, k_start=k_start)
+    assert np.all((np.abs(wide(again) - ref) <= HALF["bf16"] * (np.abs(ref) + size) * 1.01 + 4e-4 * size)[:rows])
