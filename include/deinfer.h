@@ -505,7 +505,8 @@ int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_he
  * Arithmetic as of deinfer_tree_attention: fp32 throughout, probabilities rounded to the storage type for the second product, their
  * sum that of the rounded ones, one rounding of the output.  Results do not depend on timing.  The workspace
  * (deinfer_prompt_attention_workspace_bytes, host only; 256-byte aligned) needs no clearing and serves one call at a time; its size is that of
- * the call's own T and n_seqs.  T, n_keys <= 2^28, at most DEINFER_KV_MAX_SEQS sequences.
+ * the call's own T and n_seqs.  T, n_keys <= 2^28, at most DEINFER_KV_MAX_SEQS sequences.  Tiles have one height for all sequences, by the
+ * mean T / n_seqs: long chunks beside many single tokens are faster in a call of their own.
  */
 #define DEINFER_ROPE_MAX_AXES 4
 #define DEINFER_NORM_MAX_DIM 2048

@@ -9,8 +9,10 @@
 // with the pair (i, i + rot_dim / 2) of a head, or (2 i, 2 i + 1) where pairs are interleaved; the elements from
 // rot_dim on are normed only, values are copied.  Everything between the load and the store is fp32, with one rounding.  Bound by HBM:
 // every element is read once and written once.  A workgroup has a row, as many lanes as a head has pieces a head, so that its sum of squares is a
-// few exchanges between lanes and the row's cosines and sines are formed once.  8191 rows of 96 heads of 128, fp16: 402 MB in 78 us, 5.2 TB/s;
-// 16000 rows of 80 heads of 128, three axes, bf16: 656 MB in 122 us, 5.4 TB/s (a copy of 1 GiB: 5.0); 8 rows 6.5 us, latency.
+// few exchanges between lanes and the row's cosines and sines are formed once.  Calls one after another: 8191 rows of 96 heads of 128, fp16, 403 MB in
+// 78 us, 5.2 TB/s; fp32, 805 MB in 161, 5.0; 16000 rows of 80 heads of 128, three axes, bf16, 656 MB in 122, 5.4 (copies of 200 to 500 MiB: 5.3 to
+// 5.4).  Each kernel by itself, as a trace has them: 85 and 132 us for the 16-bit ones.  8 rows 5.8 us in a graph, the rotary store alone 3.5:
+// latency, the sum's exchanges and behind them the weights' load.
 #pragma once
 #include "rope_store_kernel.h"
 

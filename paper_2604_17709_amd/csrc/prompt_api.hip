@@ -41,8 +41,10 @@ PromptPlan prompt_plan(int64_t T, int64_t n_seqs, int64_t n_q, int64_t n_kv, int
   PromptPlan p;
   const int64_t per_head = ceil_div(T * (n_q / n_kv), n_seqs > 0 ? n_seqs : 1);      // rows of a sequence and key head, on average
   // Tiles of 16 rows without LDS, of 128 and of 256, in us, heads of 128, 8 key heads.  8 query heads each, 4000 keys: 8 sequences with one
-  // token 30.9, 36.8 and 37.5, with two 32.4 and 38.6; 64 with one 201, 191 and 191, with two 205 and 193, with three (two tiles of 16)
-  // 390 and 193.  4 query heads each, whole prompts: 32 of 8 tokens 13.4, 15.1 and 16.3, 32 of 16 15.1, 15.4 and 16.7; from 64 tokens on
+  // token 30.9, 36.8 and 37.5, with two 32.4 and 38.6; 16 with one 49 and (256 rows) 54, 32 107 and 108; 64 with one 201, 191 and 191, with
+  // two 205 and 193, with three (two tiles of 16) 390 and 193: up to 16 rows the rule takes the small tiles whatever the sequences' number,
+  // which is 5 to 6 % too slow for 64 and more.  One height for all sequences: a chunk of 512 tokens beside 63 single ones, 32 heads
+  // each with its own keys, 2000 to 4096 of them, gets 16 rows, 698 us where two calls take 68 and 520.  4 query heads each, whole prompts: 32 of 8 tokens 13.4, 15.1 and 16.3, 32 of 16 15.1, 15.4 and 16.7; from 64 tokens on
   // the last two are equal, and long ones need 256 rows (906 TFLOP/s against 746).
   p.rows = per_head <= 16 ? 16 : head_dim > 128 || per_head <= 128 ? 128 : 256;
   p.cols = p.rows == 16 ? (head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256) : head_dim <= 64 ? 64 : head_dim <= 96 ? 96 : head_dim <= 128 ? 128 : 256;

@@ -523,13 +523,14 @@ __global__ __launch_bounds__(ATT_THREADS) void prompt_rows_kernel(const PromptPa
 // Bound by the issue of one wavefront's instructions: a turn of heads of 128 has 16 products of 32 cycles and 78 vector instructions, of which 16
 // are exponentials, and a product hides about five of them (three beside an exponential).  So the products of the turn before run beside the
 // probabilities, the next scores beside the sum and the reads of V, in a fixed order, and registers hold 32 rows: with 64 rows per
-// wavefront (half the reads from LDS) 970 TFLOP/s in place of 1015, with two groups of wavefronts in opposite halves of a turn 950.
+// wavefront (half the reads from LDS) 970 TFLOP/s, with two groups of wavefronts in opposite halves of a turn 950, both when this form was at 1015.
 //   one prompt of 16384 tokens, 64 query and 8 key heads of 128, bf16     4.40 TFLOP    4.0 ms    1100 TFLOP/s (a large library product: 1210)
-//   16 of 1250 .. 2500, 32 heads of 128, fp16                             0.53          0.78      680
-//   4 of 3500 .. 6000, windows of 1024, 16 query and 8 key heads of 256   0.30          0.46      660
-//   24 images of 700 .. 1024 patches, 16 heads of 80, fp16                0.067         0.16      420
-// In the first the matrix units are busy for 51 % of the cycles and the clock goes down to 1.8 to 2 GHz: at that point power takes part in the bound.
-// In the others tiles have few keys (PROMPT_START), and heads of 80 have 11 products a turn for the same vector instructions.
+//   16 of 1344 .. 2500, 32 heads of 128, fp16                             0.53          0.77      684
+//   4 of 3454 .. 6000, windows of 1024, 16 query and 8 key heads of 256   0.30          0.46      661
+//   24 images of 532 .. 1024 patches, 16 heads of 80, fp16                0.067         0.16      420
+// In the first the matrix units are busy for 53 % of the cycles and the clock goes down to 1.8 to 2 GHz: at that point power takes part in the bound.
+// In the others tiles have few keys: PROMPT_START, what a tile costs beside them, is 18 to 23 % of the work.  Heads of 80 have 11 products a turn (352
+// cycles) for the same vector instructions (about 500): the matrix units are busy for 26 % of the cycles.
 // KS: 16-feature steps of the first product (padded head dimension 16 KS); PITCH: features of a row in LDS.
 template <int KS_, int WAVES_> struct PromptTile {
   static constexpr int KS = KS_, WAVES = WAVES_;
