@@ -493,8 +493,9 @@ int deinfer_tree_attention(const void *q, int64_t T, int64_t ldq, int64_t n_q_he
  *   q_start, k_start: device int32 [n_seqs + 1]: first row of every sequence in q and out, in k and v, and the end of the last; k_start
  *                   NULL: q_start.  What lies outside the tensors is cut off; sequences do not share rows of out (the lists do not
  *                   decrease).  A sequence's keys end where the next one's begin.  Where there is a gap between, as in a buffer of
- *                   deinfer_kv_compact_copy, in which every sequence begins at a block, the gap is a sequence of its own, with no
- *                   rows: q_start {.., r, r', r', ..}, k_start {.., first key, last key + 1, the next one's first key, ..}.  Row i of a sequence with n rows and m keys stands at p = m - n + i (the last row at the last key)
+ *                   deinfer_kv_compact_copy, in which every sequence begins at a block, the gap is a sequence of its own, counted
+ *                   in n_seqs, with no rows: q_start {.., r, r', r', ..}, k_start {.., first key, last key + 1, the next one's first
+ *                   key, ..}.  Row i of a sequence with n rows and m keys stands at p = m - n + i (the last row at the last key)
  *                   and sees its keys j, p - left <= j <= p + right; a negative side has no bound (causal: left = -1, right = 0).  A row that sees
  *                   no key gives zeros; so does one whose scores are all minus infinity.  What a row does not see has no
  *                   influence, infinities and NaN included.  An infinite value that it sees makes an infinity, or no number where
